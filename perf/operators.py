@@ -88,6 +88,12 @@ def _padded(cols):
     return -(-cols // 128) * 128
 
 
+def _power(e):
+    """2^e in 32 bits from its exponent field, e from -126 to 127 (-127: zero).  torch.ldexp goes by pow, which is a rounding off
+    at some exponents, and that moves values that lie half way between two elements."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
 def _plain_quantize(x):
     """(q, s) of the rows of x."""
     rows, cols = x.shape
@@ -95,7 +101,7 @@ def _plain_quantize(x):
     most = b.abs().amax(-1, keepdim=True)
     shared = (torch.frexp(most).exponent - 3).clamp(-127, 127)
     shared = torch.where(most == 0, torch.full_like(shared, -127), shared)
-    v = torch.ldexp(b.abs(), -shared)
+    v = b.abs() * _power(-shared)
     code = torch.signbit(b).to(torch.uint8) * 8
     for at, ties_up in ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False), (3.5, True), (5.0, False)):
         code += (v >= at) if ties_up else (v > at)
@@ -108,7 +114,7 @@ def _plain_values(q, s, cols):
     table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float32, device=q.device)
     table = torch.cat((table, -table))
     code = torch.stack((q & 15, q >> 4), -1).view(q.shape[0], -1, 32).int()
-    v = torch.ldexp(table[code], s.int().unsqueeze(-1) - 127)
+    v = table[code] * _power(s.int().unsqueeze(-1) - 127)
     return v.view(q.shape[0], -1)[:, :cols]
 
 
