@@ -46,7 +46,8 @@
 extern "C" {
 #endif
 
-typedef enum { DLA_F64 = 0, DLA_F32 = 1 } dla_dtype;
+/* DLA_BF16 and DLA_F16 are for the mx4_ entry points, which in turn do not take DLA_F64. */
+typedef enum { DLA_F64 = 0, DLA_F32 = 1, DLA_BF16 = 2, DLA_F16 = 3 } dla_dtype;
 
 enum {
   DLA_SUCCESS = 0,
@@ -58,6 +59,8 @@ enum {
 
 /* Kernel selectors for dla_default_params(). */
 enum { DLA_KERNEL_MM3 = 0, DLA_KERNEL_LU = 1, DLA_KERNEL_CHOLESKY = 2 };
+/* Kernel selectors for mx4_default_params() and mx4_enumerate_tiles(). */
+enum { DLA_KERNEL_MX4_GEMM = 3, DLA_KERNEL_MX4_APPLY = 4 };
 
 /*
  * Schedule of one GEMM.  tile_m x tile_n is the macro-tile one workgroup
@@ -284,6 +287,86 @@ int dla_gemm_choice(int op, int64_t lda, int64_t ldb, int64_t m, int64_t n, int6
  */
 int dla_rank_update(int lower, const void* d_l, const void* d_r, void* d_c, int64_t ld, int64_t m, int64_t k,
                     dla_dtype dt, void* hip_stream);
+
+/*
+ * Microscaled 4-bit floating point (the MX formats of the Open Compute Project, version 1.0: E2M1 elements, one E8M0 scale
+ * per block of 32): the form in which a language model's weights, and in training its activations and gradients, are
+ * multiplied on this card's scaled matrix instructions.  Beside dla_gemm these are the library's low-precision products;
+ * their schedules are call parameters in the same way.
+ *
+ * A microscaled matrix of `rows` x `cols` is two byte arrays:
+ *   q   row r starts at r * ldq bytes.  Byte j holds the elements of columns 2j (lower four bits) and 2j + 1.  An element is a
+ *       sign, two bits of exponent and one of mantissa: +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}.
+ *   s   row r starts at r * lds bytes.  Byte b is the scale of columns 32b .. 32b + 31: 2^(s - 127), and 255 a NaN.
+ * The columns are padded to a multiple of 128, P = mx4_padded(cols): rows hold P / 2 and P / 32 bytes, and the padding has to be
+ * zero in both arrays, as mx4_quantize leaves it (the products run over it).  q and ldq are multiples of 16, s and lds of
+ * 4 (bytes); ldq >= P / 2, lds >= P / 32, both at most 2^22 (a longer row is refused with DLA_ERR_TOO_LARGE).
+ * Outputs must not overlap inputs or each other.
+ */
+int64_t mx4_padded(int64_t cols); /* cols rounded up to a multiple of 128; 0 for a negative one */
+
+/*
+ * The microscaled form of X (rows x cols, DLA_F32, DLA_BF16 or DLA_F16, row-major, leading dimension ldx in elements), of its
+ * transpose, or both in one pass over X: a training step multiplies each of x, W and dy once along its rows and once along
+ * its columns.  A block's scale is the power of two 2^(floor(log2(max |x|)) - 2), at least 2^-127; an element is x over the scale
+ * rounded to the nearest value, ties to the even mantissa, and magnitudes above 6 to 6 (a sign is kept where the
+ * value rounds to zero).  A block that holds an infinity or a NaN is a NaN as a whole: scale 255, elements 0.  A block of
+ * zeros has scale 0.
+ *   d_q, ldq, d_s, lds       the form of X (rows x cols, blocks along the columns), or d_q and d_s both NULL
+ *   d_qt, ldqt, d_st, ldst   the form of X^T (cols x rows, blocks along the rows of X), or both NULL; one of the two is needed
+ */
+int mx4_quantize(const void* d_x, int64_t ldx, int64_t rows, int64_t cols, dla_dtype dt, void* d_q, int64_t ldq, void* d_s,
+                 int64_t lds, void* d_qt, int64_t ldqt, void* d_st, int64_t ldst, void* hip_stream);
+
+/*
+ * Y = the values of a microscaled matrix, rounded once to Y's type (DLA_F32 and DLA_BF16 hold them all but the ones of scales
+ * from 2^126 on, which become infinite beyond the type's range; DLA_F16 has infinities from 65520 on and loses bits below 2^-14).
+ */
+int mx4_dequantize(const void* d_q, int64_t ldq, const void* d_s, int64_t lds, int64_t rows, int64_t cols, dla_dtype dt,
+                   void* d_y, int64_t ldy, void* hip_stream);
+
+/*
+ * Schedule of a product.  tile_m x tile_n: the part of the result one workgroup computes, from the menu of
+ * mx4_enumerate_tiles (both 0: the library's choice by the sizes).  splits: how many workgroups share one tile along the sum
+ * (1 .. 32, at most one per 128 terms of the sum; 0: the library's choice); their sums are added in a fixed order by a second launch.
+ */
+typedef struct {
+  int tile_m, tile_n, splits;
+} mx4_params;
+
+/*
+ * op 0: C = A*B^T, op 1: C += A*B^T; A m x k and B n x k microscaled, C m x n in DLA_F32, DLA_BF16 or DLA_F16 with leading
+ * dimension ldc in elements.  Products are exact and summed in fp32 by the scaled matrix instructions; C is rounded once.
+ * With the two forms of mx4_quantize this is a linear layer's forward pass, y = x W^T, and its gradients, dx = dy (W^T)^T and
+ * dw = dy^T (x^T)^T.  k == 0 is a sum of nothing.
+ *   d_workspace / workspace_bytes   at least mx4_gemm_workspace_bytes(...) bytes, 256-byte aligned (0 bytes: may be NULL).
+ *                                   Calls that may run at the same time need one each.
+ */
+int mx4_gemm(int op, const void* d_a, int64_t lda, const void* d_sa, int64_t ldsa, const void* d_b, int64_t ldb,
+             const void* d_sb, int64_t ldsb, void* d_c, int64_t ldc, int64_t m, int64_t n, int64_t k, dla_dtype dt,
+             const mx4_params* p, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+size_t mx4_gemm_workspace_bytes(int64_t m, int64_t n, int64_t k, const mx4_params* p);
+
+/*
+ * Microscaled weights W (n x k) applied to rows X in ordinary floating point:
+ *   op 0:  Y = X*W^T   X m x k, Y m x n   (a linear layer)
+ *   op 1:  Y = X*W     X m x n, Y m x k   (its gradient with respect to its input, the weights frozen)
+ * X in dt and Y in dt_y, each DLA_F32, DLA_BF16 or DLA_F16.  Nothing of X or W is rounded: X goes into the bf16 matrix
+ * instructions as one (DLA_BF16), two (DLA_F16) or three (DLA_F32) bf16 terms that add up to it (DLA_F32: down to 2^-133);
+ * sums are fp32, Y is rounded once.  Workspace as for mx4_gemm.
+ */
+int mx4_apply(int op, const void* d_x, int64_t ldx, dla_dtype dt, const void* d_w, int64_t ldw, const void* d_sw, int64_t ldsw,
+              void* d_y, int64_t ldy, dla_dtype dt_y, int64_t m, int64_t n, int64_t k, const mx4_params* p,
+              void* d_workspace, size_t workspace_bytes, void* hip_stream);
+size_t mx4_apply_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const mx4_params* p);
+
+/*
+ * The menu and the library's choice, for a search: kernel is DLA_KERNEL_MX4_GEMM or DLA_KERNEL_MX4_APPLY.  mx4_enumerate_tiles
+ * writes up to cap tiles for op (splits 0) and returns how many there are; mx4_default_params fills in the schedule that a call
+ * without one runs (queries on the host, no GPU needed).
+ */
+int mx4_enumerate_tiles(int kernel, int op, mx4_params* out, int cap);
+int mx4_default_params(int kernel, int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, mx4_params* out);
 
 /* 1 if the schedule is in the menu for dt (fields equal to 0 are filled with defaults first), else 0. */
 int dla_gemm_params_supported(dla_dtype dt, const dla_gemm_params* p);

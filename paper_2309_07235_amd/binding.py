@@ -19,9 +19,10 @@ import torch  # noqa: F401
 _HERE = Path(__file__).resolve().parent
 LIB_PATH = _HERE / "libdla_mi355x.so"
 
-DLA_F64, DLA_F32 = 0, 1
+DLA_F64, DLA_F32, DLA_BF16, DLA_F16 = 0, 1, 2, 3
 DLA_SUCCESS, DLA_ERR_UNSUPPORTED_PARAMS, DLA_ERR_WORKSPACE, DLA_ERR_HIP, DLA_ERR_TOO_LARGE = 0, 1, 2, 3, 4
 DLA_KERNEL_MM3, DLA_KERNEL_LU, DLA_KERNEL_CHOLESKY = 0, 1, 2
+DLA_KERNEL_MX4_GEMM, DLA_KERNEL_MX4_APPLY = 3, 4
 OP_ASSIGN, OP_SUB, OP_SUB_NT_LOWER = 0, 1, 2
 PHASE_GEMM, PHASE_DIAG, PHASE_TRSM, PHASE_UPDATE = 0, 1, 2, 3
 
@@ -45,6 +46,16 @@ class FactorParams(ctypes.Structure):
 
 class Mm3Params(ctypes.Structure):
     _fields_ = [("e", GemmParams), ("f", GemmParams), ("g", GemmParams)]
+
+
+class Mx4Params(ctypes.Structure):
+    _fields_ = [("tile_m", ctypes.c_int), ("tile_n", ctypes.c_int), ("splits", ctypes.c_int)]
+
+    def as_tuple(self):
+        return (self.tile_m, self.tile_n, self.splits)
+
+    def __repr__(self):
+        return "Mx4Params(tile=%dx%d, splits=%d)" % self.as_tuple()
 
 
 class DlaError(RuntimeError):
@@ -117,6 +128,25 @@ def _load() -> ctypes.CDLL:
     lib.dla_profile_read.argtypes = [ci, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64),
                                      ctypes.POINTER(ctypes.c_double)]
     lib.dla_profile_read.restype = ci
+    mxp = ctypes.POINTER(Mx4Params)
+    lib.mx4_padded.argtypes = [i64]
+    lib.mx4_padded.restype = i64
+    lib.mx4_quantize.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.mx4_quantize.restype = ci
+    lib.mx4_dequantize.argtypes = [vp, i64, vp, i64, i64, i64, ci, vp, i64, vp]
+    lib.mx4_dequantize.restype = ci
+    lib.mx4_gemm.argtypes = [ci, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, ci, mxp, vp, sz, vp]
+    lib.mx4_gemm.restype = ci
+    lib.mx4_gemm_workspace_bytes.argtypes = [i64, i64, i64, mxp]
+    lib.mx4_gemm_workspace_bytes.restype = sz
+    lib.mx4_apply.argtypes = [ci, vp, i64, ci, vp, i64, vp, i64, vp, i64, ci, i64, i64, i64, mxp, vp, sz, vp]
+    lib.mx4_apply.restype = ci
+    lib.mx4_apply_workspace_bytes.argtypes = [ci, i64, i64, i64, ci, mxp]
+    lib.mx4_apply_workspace_bytes.restype = sz
+    lib.mx4_enumerate_tiles.argtypes = [ci, ci, mxp, ci]
+    lib.mx4_enumerate_tiles.restype = ci
+    lib.mx4_default_params.argtypes = [ci, ci, i64, i64, i64, ci, mxp]
+    lib.mx4_default_params.restype = ci
     lib.dla_strerror.argtypes = [ci]
     lib.dla_strerror.restype = ctypes.c_char_p
     lib.dla_last_error_detail.argtypes = []
@@ -353,6 +383,147 @@ def dla_gemm(op: int, a, b, c, p: GemmParams | None = None, stream=None):
     (ap, lda), (bp, ldb), (cp, ldc) = _matrix(a, "a"), _matrix(b, "b"), _matrix(c, "c")
     _check(lib.dla_gemm(op, ap, lda, bp, ldb, cp, ldc, m, n, k, dt, _ref(p), ctypes.c_void_p(_stream_ptr(stream))),
            "dla_gemm")
+
+
+_MX4_DTYPES = {torch.float32: DLA_F32, torch.bfloat16: DLA_BF16, torch.float16: DLA_F16}
+
+
+def _mx4_dtype(t) -> int:
+    code = _MX4_DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
+
+
+class Mx4:
+    """A microscaled matrix as two uint8 device tensors: q (rows x at least padded / 2) and s (rows x at least padded / 32);
+    see dla.h for their layout.  cols is the number of columns without the padding."""
+    __slots__ = ("q", "s", "cols")
+
+    def __init__(self, q, s, cols: int):
+        self.q, self.s, self.cols = q, s, int(cols)
+
+    @property
+    def rows(self) -> int:
+        return self.q.shape[0]
+
+    def _args(self, name):
+        q, s, wide = self.q, self.s, mx4_padded(self.cols)
+        if q.dim() != 2 or s.dim() != 2 or q.dtype != torch.uint8 or s.dtype != torch.uint8 or s.shape[0] != q.shape[0]:
+            raise ValueError(f"{name}: q and s must be uint8 matrices with the same number of rows")
+        if self.cols < 0 or q.shape[1] * 2 < wide or s.shape[1] * 32 < wide:
+            raise ValueError(f"{name}: q and s must hold {wide} columns (mx4_padded({self.cols}))")
+        return (*_matrix(q, name), *_matrix(s, name))
+
+
+def mx4_padded(cols: int) -> int:
+    """The columns that a row of a microscaled matrix holds, padding included (see dla.h: mx4_padded)."""
+    return -(-cols // 128) * 128
+
+
+def mx4_empty(rows: int, cols: int, device="cuda") -> Mx4:
+    """Room for a microscaled matrix, to be filled by mx4_quantize."""
+    wide = mx4_padded(cols)
+    return Mx4(torch.empty((rows, wide // 2), dtype=torch.uint8, device=device),
+               torch.empty((rows, wide // 32), dtype=torch.uint8, device=device), cols)
+
+
+def _mx4_call(fn, name, stream, tensors, args):
+    """fn(*args, stream) on the device that holds the tensors."""
+    device = tensors[0].device
+    for t in tensors:
+        if t.device != device:
+            raise ValueError(f"{name}: tensors on different devices")
+    if device.type != "cuda":
+        raise ValueError(f"{name}: tensors must live in device memory")
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, _stream_ptr(stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream_ptr(stream))
+    _check(rc, name)
+
+
+def mx4_quantize(x, q: Mx4 | None = None, qt: Mx4 | None = None, stream=None):
+    """The microscaled form of the device matrix x into q, of its transpose into qt; either may be None (see dla.h: mx4_quantize)."""
+    if q is None and qt is None:
+        raise ValueError("mx4_quantize: neither q nor qt")
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    tensors, args = [x], [xp, ldx, rows, cols, _mx4_dtype(x)]
+    for name, form, want in (("q", q, (rows, cols)), ("qt", qt, (cols, rows))):
+        if form is None:
+            args += [None, 0, None, 0]
+            continue
+        if (form.rows, form.cols) != want:
+            raise ValueError(f"mx4_quantize: {name} must be {want[0]} x {want[1]}")
+        args += form._args(name)
+        tensors += [form.q, form.s]
+    _mx4_call(lib.mx4_quantize, "mx4_quantize", stream, tensors, args)
+
+
+def mx4_dequantize(q: Mx4, y, stream=None):
+    """y = the values of q, rounded to y's type (see dla.h: mx4_dequantize)."""
+    if tuple(y.shape) != (q.rows, q.cols):
+        raise ValueError("mx4_dequantize: q and y differ in shape")
+    _mx4_call(lib.mx4_dequantize, "mx4_dequantize", stream, (q.q, q.s, y),
+              (*q._args("q"), q.rows, q.cols, _mx4_dtype(y), *_matrix(y, "y")))
+
+
+def _mx4_workspace(need: int, device, workspace, stream):
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        with torch.cuda.stream(stream):  # memory of the stream that uses it (None: the current one)
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def mx4_gemm(op: int, a: Mx4, b: Mx4, c, p: Mx4Params | None = None, workspace=None, stream=None):
+    """c = a*b^T (op 0) or c += a*b^T (op 1), both operands microscaled (see dla.h: mx4_gemm).  Returns the workspace it used
+    (None where the schedule needs none)."""
+    m, n, k = a.rows, b.rows, a.cols
+    if b.cols != k or tuple(c.shape) != (m, n):
+        raise ValueError("mx4_gemm: shapes do not chain")
+    pr = _ref(p)
+    need = lib.mx4_gemm_workspace_bytes(m, n, k, pr) if workspace is None else 0
+    ws, wsp, wsb = _mx4_workspace(need, c.device, workspace, stream)
+    tensors = (c, a.q, a.s, b.q, b.s) if ws is None else (c, a.q, a.s, b.q, b.s, ws)
+    _mx4_call(lib.mx4_gemm, "mx4_gemm", stream, tensors,
+              (op, *a._args("a"), *b._args("b"), *_matrix(c, "c"), m, n, k, _mx4_dtype(c), pr, wsp, wsb))
+    return ws
+
+
+def mx4_apply(op: int, x, w: Mx4, y, p: Mx4Params | None = None, workspace=None, stream=None):
+    """y = x*w^T (op 0) or y = x*w (op 1) with microscaled w (see dla.h: mx4_apply).  Returns the workspace it used (None where
+    the schedule needs none)."""
+    if op not in (0, 1):
+        raise ValueError("mx4_apply: op must be 0 or 1")
+    m, n, k = x.shape[0], w.rows, w.cols
+    terms, out = (k, n) if op == 0 else (n, k)
+    if x.dim() != 2 or x.shape[1] != terms or tuple(y.shape) != (m, out):
+        raise ValueError("mx4_apply: shapes do not chain")
+    pr, dt = _ref(p), _mx4_dtype(x)
+    need = lib.mx4_apply_workspace_bytes(op, m, n, k, dt, pr) if workspace is None else 0
+    ws, wsp, wsb = _mx4_workspace(need, y.device, workspace, stream)
+    tensors = (x, w.q, w.s, y) if ws is None else (x, w.q, w.s, y, ws)
+    _mx4_call(lib.mx4_apply, "mx4_apply", stream, tensors,
+              (op, *_matrix(x, "x"), dt, *w._args("w"), *_matrix(y, "y"), _mx4_dtype(y), m, n, k, pr, wsp, wsb))
+    return ws
+
+
+def mx4_enumerate_tiles(kernel: int, op: int = 0):
+    n = lib.mx4_enumerate_tiles(kernel, op, None, 0)
+    arr = (Mx4Params * n)()
+    lib.mx4_enumerate_tiles(kernel, op, arr, n)
+    return [Mx4Params(*a.as_tuple()) for a in arr]
+
+
+def mx4_default_params(kernel: int, op: int, m: int, n: int, k: int, dtype_code: int = DLA_BF16) -> Mx4Params:
+    """The schedule that a call without one runs (see dla.h: mx4_default_params)."""
+    out = Mx4Params()
+    _check(lib.mx4_default_params(kernel, op, m, n, k, dtype_code, ctypes.byref(out)), "mx4_default_params")
+    return out
 
 
 def dla_rank_update(lower: bool, l, r, c, stream=None):

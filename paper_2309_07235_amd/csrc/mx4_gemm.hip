@@ -1,0 +1,62 @@
+// Host side of the microscaled product: its tile menu, the choice of a schedule and the launch.
+#include "mx4_gemm_kernel.hpp"
+#include "mx4_host.hpp"
+
+namespace dla {
+namespace {
+
+struct Tile {
+  int m, n;
+};
+const Tile kTiles[] = {{16, 16}, {32, 32}};
+constexpr int kNumTiles = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
+constexpr int kMaxSplits = 32;
+
+int steps_of(int64_t k) { return (int)((k + kMxStep - 1) / kMxStep); }
+
+template <int MB, int NB, typename T>
+int launch_direct(const MxGemmArgs& g, hipStream_t stream) {
+  hipLaunchKernelGGL((mx4_gemm_direct_kernel<MB, NB, T>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(kMxDirectWaves * 64), 0,
+                     stream, g);
+  return launch_status(__func__);
+}
+
+template <typename T>
+int launch_typed(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
+  if (plan.tile_m == 16) return launch_direct<1, 1, T>(g, stream);
+  return launch_direct<2, 2, T>(g, stream);
+}
+
+}  // namespace
+
+int mx4_gemm_menu(mx4_params* out, int cap) {
+  for (int i = 0; i < kNumTiles && i < cap && out; ++i) out[i] = mx4_params{kTiles[i].m, kTiles[i].n, 0};
+  return kNumTiles;
+}
+
+int mx4_gemm_plan(int64_t m, int64_t n, int64_t k, const mx4_params* p, MxPlan* plan) {
+  MxPlan r = {0, 0, 0};
+  if (p) r = MxPlan{p->tile_m, p->tile_n, p->splits};
+  if (r.tile_m < 0 || r.tile_n < 0 || r.splits < 0 || r.splits > kMaxSplits || r.splits > steps_of(k)) return DLA_ERR_UNSUPPORTED_PARAMS;
+  if (r.tile_m == 0 && r.tile_n == 0) r.tile_m = r.tile_n = m <= 16 ? 16 : 32;
+  bool found = false;
+  for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n;
+  if (!found) return DLA_ERR_UNSUPPORTED_PARAMS;
+  if (r.splits == 0) r.splits = 1;
+  const int64_t tiles = ((m + r.tile_m - 1) / r.tile_m) * ((n + r.tile_n - 1) / r.tile_n);
+  if (tiles * r.splits > 0x7fffffff) return DLA_ERR_TOO_LARGE;
+  *plan = r;
+  return DLA_SUCCESS;
+}
+
+int mx4_gemm_launch(bool onto, const Mx4View& a, const Mx4View& b, void* c, int64_t ldc, int64_t k, dla_dtype dt, const MxPlan& plan,
+                    float* parts, hipStream_t stream) {
+  const MxGemmArgs g = {a, b, c, parts, ldc, steps_of(k), plan.splits, (a.rows + plan.tile_m - 1) / plan.tile_m,
+                        (b.rows + plan.tile_n - 1) / plan.tile_n, onto};
+  const int rc = dt == DLA_F32 ? launch_typed<float>(g, plan, stream)
+                 : dt == DLA_BF16 ? launch_typed<__bf16>(g, plan, stream) : launch_typed<_Float16>(g, plan, stream);
+  if (rc != DLA_SUCCESS || plan.splits == 1) return rc;
+  return mx4_join_launch(parts, plan.splits, a.rows, b.rows, c, ldc, dt, onto, stream);
+}
+
+}  // namespace dla
