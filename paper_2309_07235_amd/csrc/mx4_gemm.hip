@@ -8,7 +8,7 @@ namespace {
 struct Tile {
   int m, n;
 };
-const Tile kTiles[] = {{16, 16}, {32, 32}};
+const Tile kTiles[] = {{16, 16}, {32, 32}, {128, 128}, {256, 256}};
 constexpr int kNumTiles = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
 constexpr int kMaxSplits = 32;
 
@@ -21,10 +21,19 @@ int launch_direct(const MxGemmArgs& g, hipStream_t stream) {
   return launch_status(__func__);
 }
 
+template <int TM, int TN, int WM, int WN, typename T>
+int launch_tile(const MxGemmArgs& g, hipStream_t stream) {
+  hipLaunchKernelGGL((mx4_gemm_tile_kernel<TM, TN, WM, WN, T>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(WM * WN * 64), 0, stream,
+                     g);
+  return launch_status(__func__);
+}
+
 template <typename T>
 int launch_typed(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
   if (plan.tile_m == 16) return launch_direct<1, 1, T>(g, stream);
-  return launch_direct<2, 2, T>(g, stream);
+  if (plan.tile_m == 32) return launch_direct<2, 2, T>(g, stream);
+  if (plan.tile_m == 128) return launch_tile<128, 128, 2, 2, T>(g, stream);
+  return launch_tile<256, 256, 2, 4, T>(g, stream);
 }
 
 }  // namespace
@@ -38,7 +47,7 @@ int mx4_gemm_plan(int64_t m, int64_t n, int64_t k, const mx4_params* p, MxPlan* 
   MxPlan r = {0, 0, 0};
   if (p) r = MxPlan{p->tile_m, p->tile_n, p->splits};
   if (r.tile_m < 0 || r.tile_n < 0 || r.splits < 0 || r.splits > kMaxSplits || r.splits > steps_of(k)) return DLA_ERR_UNSUPPORTED_PARAMS;
-  if (r.tile_m == 0 && r.tile_n == 0) r.tile_m = r.tile_n = m <= 16 ? 16 : 32;
+  if (r.tile_m == 0 && r.tile_n == 0) r.tile_m = r.tile_n = m <= 16 ? 16 : m < 128 ? 32 : m < 2048 ? 128 : 256;
   bool found = false;
   for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n;
   if (!found) return DLA_ERR_UNSUPPORTED_PARAMS;

@@ -87,4 +87,143 @@ __global__ void __launch_bounds__(kMxDirectWaves * 64) mx4_gemm_direct_kernel(Mx
   }
 }
 
+// Tile `id` of a grid of tiles: eight rows of tiles are walked column by column, so that the workgroups of an XCD, which are
+// neighbours in id, share operands in its L2.
+__device__ __forceinline__ void tile_at(int id, int tiles_m, int tiles_n, int* ti, int* tj) {
+  const int band = 8 * tiles_n, first = id / band * 8, height = min(8, tiles_m - first), in = id % band;
+  *ti = first + in % height;
+  *tj = in / height;
+}
+
+template <int TM, int TN, int WM, int WN, typename T>
+__global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g) {
+  constexpr int NT = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
+  constexpr int LA = TM * 4 / NT, LB = TN * 4 / NT;  // loads of 16 bytes per thread and step
+  static_assert(TM + TN == NT, "one thread per row loads its scales");
+  constexpr int STAGE = (TM + TN) * 4;               // a step's rows of both operands, in units of 16 bytes
+  __shared__ u32x4_t rows[4 * STAGE];
+  __shared__ u32x4_t scales[2][TM + TN];             // those of four steps at a time, 16 bytes a row
+  const int tiles = g.tiles_m * g.tiles_n;
+  const int split = (int)blockIdx.x / tiles;
+  int ti, tj;
+  tile_at(xcd_contiguous_id((int)blockIdx.x % tiles, tiles), g.tiles_m, g.tiles_n, &ti, &tj);
+  const int m0 = ti * TM, n0 = tj * TN;
+  const int first = (int)((int64_t)g.steps * split / g.splits), steps = (int)((int64_t)g.steps * (split + 1) / g.splits) - first;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l31 = lane & 31, l5 = lane >> 5;
+  const int wm0 = wave / WN * (TM / WM), wn0 = wave % WN * (TN / WN);
+
+  // A load instruction fills 16 rows of 64 bytes; chunk c of row r lies at c ^ (r / 4) % 4, so that the 16 rows which a read of 16
+  // lanes takes lie in all banks.  Rows past the last repeat it.
+  const uint8_t* const aq = g.a.q + (int64_t)m0 * g.a.ldq + (int64_t)first * 64;
+  const uint8_t* const bq = g.b.q + (int64_t)n0 * g.b.ldq + (int64_t)first * 64;
+  unsigned int off[LA + LB];
+#pragma unroll
+  for (int i = 0; i < LA + LB; ++i) {
+    const int r = i < LA ? (wave * LA + i) * 16 + lane / 4 : (wave * LB + i - LA) * 16 + lane / 4;
+    const int c = (lane & 3) ^ ((r >> 2) & 3);
+    off[i] = (unsigned int)(i < LA ? min(r, g.a.rows - 1 - m0) * (int)g.a.ldq : min(r, g.b.rows - 1 - n0) * (int)g.b.ldq) + c * 16;
+  }
+  const unsigned int lds_rows = lds_offset(rows), lds_scales = lds_offset(scales);
+  // Loads past the last step repeat it, into a stage that nobody reads any more: the number of loads in flight is then the same
+  // in every step, and a wait can count them.
+  auto load = [&](int s, int stage) {
+    const int64_t at = (int64_t)min(s, steps - 1) * 64;
+    const unsigned int to = lds_rows + stage * STAGE * 16;
+#pragma unroll
+    for (int i = 0; i < LA; ++i) load_to_lds(aq + at, off[i], to + (wave * LA + i) * 1024);
+#pragma unroll
+    for (int i = 0; i < LB; ++i) load_to_lds(bq + at, off[LA + i], to + TM * 64 + (wave * LB + i) * 1024);
+  };
+  // The scales of steps 4 chunk .. 4 chunk + 3, a thread a row (a wave's rows are all A's or all B's); moved back to begin at most
+  // four steps before the row's end.
+  const bool of_a = wave * 64 < TM;
+  const uint8_t* const sp = of_a ? g.a.s + (int64_t)m0 * g.a.lds : g.b.s + (int64_t)n0 * g.b.lds;
+  const unsigned int soff = of_a ? (unsigned int)(min(tid, g.a.rows - 1 - m0) * (int)g.a.lds) : (unsigned int)(min(tid - TM, g.b.rows - 1 - n0) * (int)g.b.lds);
+  auto scales_from = [&](int chunk) { return min(first + chunk * 4, g.steps - 4); };
+  auto load_scales = [&](int chunk) {
+    load_to_lds(sp + (int64_t)scales_from(chunk) * 4, soff, lds_scales + (chunk & 1) * (TM + TN) * 16 + wave * 1024);
+  };
+
+  f32x16_t acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+  auto multiply = [&](int s, int stage) {
+    const u32x4_t* const st = rows + stage * STAGE;
+    const unsigned int* const w = reinterpret_cast<const unsigned int*>(scales[(s >> 2) & 1]) + (g.steps >= 4 ? first + s - scales_from(s >> 2) : s);
+    int sa[FM], sb[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) sa[i] = (int)(w[(wm0 + i * 32 + l31) * 4] >> (8 * l5));
+#pragma unroll
+    for (int j = 0; j < FN; ++j) sb[j] = (int)(w[(TM + wn0 + j * 32 + l31) * 4] >> (8 * l5));
+    auto read = [&](int r, int c) { return __builtin_bit_cast(i32x4_t, st[r * 4 + (c ^ ((r >> 2) & 3))]); };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      i32x4_t a[FM], b[FN];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) a[i] = read(wm0 + i * 32 + l31, h * 2 + l5);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) b[j] = read(TM + wn0 + j * 32 + l31, h * 2 + l5);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = h == 0 ? mx_mma32<0>(a[i], b[j], acc[i][j], sa[i], sb[j]) : mx_mma32<2>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+    }
+  };
+
+  if (g.steps >= 4) {
+    load_scales(0);
+  } else {
+    u32x4_t w = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < steps) w[i] = *reinterpret_cast<const unsigned int*>(sp + soff + (first + i) * 4);
+    scales[0][tid] = w;
+  }
+  // three steps are on their way while one is multiplied
+  constexpr int L = LA + LB;
+  load(0, 0);
+  load(1, 1);
+  load(2, 2);
+  for (int s = 0;; s += 4) {
+    wait_loads_and_barrier<2 * L>();
+    load(s + 3, 3);
+    multiply(s, 0);
+    if (s + 1 >= steps) break;
+    wait_loads_and_barrier<2 * L>();
+    if (s + 4 < steps) load_scales(s / 4 + 1);  // its buffer was last read in step s - 1; read from step s + 4 on
+    load(s + 4, 0);
+    multiply(s + 1, 1);
+    if (s + 2 >= steps) break;
+    wait_loads_and_barrier<2 * L>();
+    load(s + 5, 1);
+    multiply(s + 2, 2);
+    if (s + 3 >= steps) break;
+    wait_loads_and_barrier<2 * L>();
+    load(s + 6, 2);
+    multiply(s + 3, 3);
+    if (s + 4 >= steps) break;
+  }
+  wait_loads_and_barrier<0>();  // nothing may arrive in LDS that is another workgroup's by then
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int r = m0 + wm0 + i * 32 + 8 * (v / 4) + 4 * l5 + v % 4, c = n0 + wn0 + j * 32 + l31;
+        if (r >= g.a.rows || c >= g.b.rows) continue;
+        if (g.splits > 1) {
+          g.parts[((int64_t)split * g.a.rows + r) * g.b.rows + c] = acc[i][j][v];
+        } else {
+          T* const out = static_cast<T*>(g.c) + r * g.ldc + c;
+          *out = (T)(g.onto ? (float)*out + acc[i][j][v] : acc[i][j][v]);
+        }
+      }
+}
+
 }  // namespace dla
