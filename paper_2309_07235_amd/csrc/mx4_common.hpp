@@ -63,7 +63,8 @@ __device__ __forceinline__ f32x16_t mx_mma32(i32x4_t a, i32x4_t b, f32x16_t c, i
 // There is no register for the load to come back to; the wait state is the one between a write of M0 and its use (nothing else in
 // these kernels uses M0).
 __device__ __forceinline__ void load_to_lds(const void* base, unsigned int off, unsigned int lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
+               : "memory");
 }
 
 // Where an array in LDS starts, for load_to_lds.

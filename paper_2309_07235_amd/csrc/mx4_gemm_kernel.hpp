@@ -1,5 +1,6 @@
 // C = A*B^T and C += A*B^T with both operands in microscaled 4-bit floating point.
 #pragma once
+#include <type_traits>
 #include "mx4_common.hpp"
 
 namespace dla {
@@ -95,11 +96,77 @@ __device__ __forceinline__ void tile_at(int id, int tiles_m, int tiles_n, int* t
   *tj = in / height;
 }
 
+// A wave's part of the result, R x C in 32 x 32 blocks whose lanes hold neighbouring columns, to rows r0.. and columns c0.. of a
+// matrix of `rows` x `cols`; `lds` is the wave's own room, 1024 units of 16 bytes.  It goes through LDS as S, rounded to T (or in
+// fp32 where it is added onto C, which is rounded once), so that rows are written 16 bytes a lane.
+template <int R, int C, typename S, typename T>
+__device__ __forceinline__ void mx_store_tile(u32x4_t* lds, const f32x16_t (&acc)[R / 32][C / 32], int lane, T* c, int64_t ldc, int r0, int c0, int rows,
+                                              int cols, bool onto) {
+  constexpr int PER = 16 / (int)sizeof(S);                              // elements of 16 bytes
+  constexpr int WIDE = C * R * (int)sizeof(S) <= 16384 ? C : 16384 / (R * (int)sizeof(S));  // columns at a time
+  constexpr int CH = WIDE / PER, RPB = CH >= 16 ? 1 : 16 / CH;          // 16-byte chunks of a row; rows of 256 bytes
+  static_assert(WIDE % 32 == 0 && C % WIDE == 0, "whole blocks");
+  typedef S run_t __attribute__((ext_vector_type(PER)));
+  typedef T out_t __attribute__((ext_vector_type(PER)));
+  typedef S quad_t __attribute__((ext_vector_type(4)));
+  const int l31 = lane & 31, l5 = lane >> 5;
+  const bool vec = (uintptr_t)c % sizeof(out_t) == 0 && ldc % PER == 0;
+  // chunk c of a row lies at c ^ (r / RPB) % CH: a wave's accesses take all banks
+  auto place = [&](int r, int chunk) { return r * CH + (chunk ^ ((r / RPB) & (CH - 1))); };
+  auto in_order = [] {  // what other lanes of the wave have written
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+#pragma unroll
+  for (int p = 0; p < C / WIDE; ++p) {
+#pragma unroll
+    for (int i = 0; i < R / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < WIDE / 32; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = j * 32 + 8 * q + 4 * l5;
+          quad_t t;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) t[v] = (S)acc[i][p * (WIDE / 32) + j][4 * q + v];
+          reinterpret_cast<quad_t*>(lds + place(i * 32 + l31, col / PER))[col % PER / 4] = t;
+        }
+    in_order();
+    const int first = c0 + p * WIDE;
+#pragma unroll 4
+    for (int e = lane; e < R * CH; e += 64) {
+      const int r = e / CH, chunk = e % CH, row = r0 + r, col = first + chunk * PER;
+      const run_t t = __builtin_bit_cast(run_t, lds[place(r, chunk)]);
+      if (row >= rows || col >= cols) continue;
+      T* const out = c + (int64_t)row * ldc + col;
+      if (vec && col + PER <= cols) {
+        out_t o;
+        if (onto) {
+          o = *reinterpret_cast<const out_t*>(out);
+#pragma unroll
+          for (int v = 0; v < PER; ++v) o[v] = (T)((float)o[v] + (float)t[v]);
+        } else {
+#pragma unroll
+          for (int v = 0; v < PER; ++v) o[v] = (T)t[v];
+        }
+        *reinterpret_cast<out_t*>(out) = o;
+      } else {
+#pragma unroll
+        for (int v = 0; v < PER; ++v)
+          if (col + v < cols) out[v] = (T)(onto ? (float)out[v] + (float)t[v] : (float)t[v]);
+      }
+    }
+    in_order();
+  }
+}
+
 template <int TM, int TN, int WM, int WN, typename T>
 __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g) {
   constexpr int NT = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr int LA = TM * 4 / NT, LB = TN * 4 / NT;  // loads of 16 bytes per thread and step
   static_assert(TM + TN == NT, "one thread per row loads its scales");
+  static_assert((TM + TN) * 16 >= WM * WN * 1024, "16 KB a wave for the result");
   constexpr int STAGE = (TM + TN) * 4;               // a step's rows of both operands, in units of 16 bytes
   __shared__ u32x4_t rows[4 * STAGE];
   __shared__ u32x4_t scales[2][TM + TN];             // those of four steps at a time, 16 bytes a row
@@ -152,27 +219,49 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
-  auto multiply = [&](int s, int stage) {
+  // Operands of half a step, and a step's scales.  The result is computed transposed (B's rows are the instruction's rows), so that
+  // a lane holds neighbouring columns of C.
+  struct Half {
+    i32x4_t a[FM], b[FN];
+  };
+  struct Scales {
+    int a[FM], b[FN];
+  };
+  auto read = [&](int stage, int h) {
     const u32x4_t* const st = rows + stage * STAGE;
+    auto at = [&](int r) { return __builtin_bit_cast(i32x4_t, st[r * 4 + ((h * 2 + l5) ^ ((r >> 2) & 3))]); };
+    Half f;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) f.b[j] = at(TM + wn0 + j * 32 + l31);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) f.a[i] = at(wm0 + i * 32 + l31);
+    return f;
+  };
+  auto read_scales = [&](int s) {
     const unsigned int* const w = reinterpret_cast<const unsigned int*>(scales[(s >> 2) & 1]) + (g.steps >= 4 ? first + s - scales_from(s >> 2) : s);
-    int sa[FM], sb[FN];
+    Scales f;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) sa[i] = (int)(w[(wm0 + i * 32 + l31) * 4] >> (8 * l5));
+    for (int j = 0; j < FN; ++j) f.b[j] = (int)(w[(TM + wn0 + j * 32 + l31) * 4] >> (8 * l5));
 #pragma unroll
-    for (int j = 0; j < FN; ++j) sb[j] = (int)(w[(TM + wn0 + j * 32 + l31) * 4] >> (8 * l5));
-    auto read = [&](int r, int c) { return __builtin_bit_cast(i32x4_t, st[r * 4 + (c ^ ((r >> 2) & 3))]); };
+    for (int i = 0; i < FM; ++i) f.a[i] = (int)(w[(wm0 + i * 32 + l31) * 4] >> (8 * l5));
+    return f;
+  };
+  auto multiply = [&](const Half& f, const Scales& w, auto h) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      i32x4_t a[FM], b[FN];
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int i = 0; i < FM; ++i) a[i] = read(wm0 + i * 32 + l31, h * 2 + l5);
+      for (int j = 0; j < FN; ++j) acc[i][j] = mx_mma32<decltype(h)::value * 2>(f.b[j], f.a[i], acc[i][j], w.b[j], w.a[i]);
+    // each read between two products: with the reads in front, all waves would wait for LDS and then all for the products
 #pragma unroll
-      for (int j = 0; j < FN; ++j) b[j] = read(TM + wn0 + j * 32 + l31, h * 2 + l5);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = h == 0 ? mx_mma32<0>(a[i], b[j], acc[i][j], sa[i], sb[j]) : mx_mma32<2>(a[i], b[j], acc[i][j], sa[i], sb[j]);
+    for (int i = 0; i < FM * FN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
+    // (an empty use of the sums: what follows is not moved in front of the products)
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
 
   if (g.steps >= 4) {
@@ -184,46 +273,47 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
       if (i < steps) w[i] = *reinterpret_cast<const unsigned int*>(sp + soff + (first + i) * 4);
     scales[0][tid] = w;
   }
-  // three steps are on their way while one is multiplied
+  // Up to four steps are on their way.  The operands of the next half step are read from LDS while this one's are multiplied; in
+  // the middle of a step the waves meet: the next step has arrived, and nobody reads this one any more.
   constexpr int L = LA + LB;
   load(0, 0);
   load(1, 1);
   load(2, 2);
+  load(3, 3);
+  wait_loads_and_barrier<3 * L>();
+  Half x = read(0, 0);
+  Scales w = read_scales(0);
+  auto step = [&](int s, int stage) {
+    const Half y = read(stage, 1);
+    multiply(x, w, std::integral_constant<int, 0>());
+    wait_loads_and_barrier<2 * L>();
+    x = read((stage + 1) & 3, 0);
+    const Scales next = read_scales(min(s + 1, steps - 1));
+    multiply(y, w, std::integral_constant<int, 1>());
+    if ((s & 3) == 0 && s + 4 < steps) load_scales(s / 4 + 1);  // its buffer was last read before step s - 1's barrier
+    load(s + 4, stage);
+    w = next;
+  };
   for (int s = 0;; s += 4) {
-    wait_loads_and_barrier<2 * L>();
-    load(s + 3, 3);
-    multiply(s, 0);
+    step(s, 0);
     if (s + 1 >= steps) break;
-    wait_loads_and_barrier<2 * L>();
-    if (s + 4 < steps) load_scales(s / 4 + 1);  // its buffer was last read in step s - 1; read from step s + 4 on
-    load(s + 4, 0);
-    multiply(s + 1, 1);
+    step(s + 1, 1);
     if (s + 2 >= steps) break;
-    wait_loads_and_barrier<2 * L>();
-    load(s + 5, 1);
-    multiply(s + 2, 2);
+    step(s + 2, 2);
     if (s + 3 >= steps) break;
-    wait_loads_and_barrier<2 * L>();
-    load(s + 6, 2);
-    multiply(s + 3, 3);
+    step(s + 3, 3);
     if (s + 4 >= steps) break;
   }
-  wait_loads_and_barrier<0>();  // nothing may arrive in LDS that is another workgroup's by then
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int r = m0 + wm0 + i * 32 + 8 * (v / 4) + 4 * l5 + v % 4, c = n0 + wn0 + j * 32 + l31;
-        if (r >= g.a.rows || c >= g.b.rows) continue;
-        if (g.splits > 1) {
-          g.parts[((int64_t)split * g.a.rows + r) * g.b.rows + c] = acc[i][j][v];
-        } else {
-          T* const out = static_cast<T*>(g.c) + r * g.ldc + c;
-          *out = (T)(g.onto ? (float)*out + acc[i][j][v] : acc[i][j][v]);
-        }
-      }
+  wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
+
+  u32x4_t* const room = rows + wave * 1024;
+  if (g.splits > 1)
+    mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.a.rows * g.b.rows, g.b.rows, m0 + wm0, n0 + wn0, g.a.rows, g.b.rows,
+                                           false);
+  else if (g.onto)
+    mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, static_cast<T*>(g.c), g.ldc, m0 + wm0, n0 + wn0, g.a.rows, g.b.rows, true);
+  else
+    mx_store_tile<TM / WM, TN / WN, T>(room, acc, lane, static_cast<T*>(g.c), g.ldc, m0 + wm0, n0 + wn0, g.a.rows, g.b.rows, false);
 }
 
 }  // namespace dla
