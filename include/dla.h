@@ -363,9 +363,9 @@ size_t mx4_apply_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, dla_dt
 /*
  * The menu and the library's choice, for a search: kernel is DLA_KERNEL_MX4_GEMM or DLA_KERNEL_MX4_APPLY.  mx4_enumerate_tiles
  * writes up to cap tiles for op (splits 0) and returns how many there are; mx4_default_params fills in the schedule that a call
- * without one runs (queries on the host, no GPU needed).
+ * without one runs (queries on the host, no GPU needed).  dt is C's type for mx4_gemm and X's for mx4_apply.
  */
-int mx4_enumerate_tiles(int kernel, int op, mx4_params* out, int cap);
+int mx4_enumerate_tiles(int kernel, int op, dla_dtype dt, mx4_params* out, int cap);
 int mx4_default_params(int kernel, int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, mx4_params* out);
 
 /* 1 if the schedule is in the menu for dt (fields equal to 0 are filled with defaults first), else 0. */

@@ -143,7 +143,7 @@ def _load() -> ctypes.CDLL:
     lib.mx4_apply.restype = ci
     lib.mx4_apply_workspace_bytes.argtypes = [ci, i64, i64, i64, ci, mxp]
     lib.mx4_apply_workspace_bytes.restype = sz
-    lib.mx4_enumerate_tiles.argtypes = [ci, ci, mxp, ci]
+    lib.mx4_enumerate_tiles.argtypes = [ci, ci, ci, mxp, ci]
     lib.mx4_enumerate_tiles.restype = ci
     lib.mx4_default_params.argtypes = [ci, ci, i64, i64, i64, ci, mxp]
     lib.mx4_default_params.restype = ci
@@ -512,10 +512,10 @@ def mx4_apply(op: int, x, w: Mx4, y, p: Mx4Params | None = None, workspace=None,
     return ws
 
 
-def mx4_enumerate_tiles(kernel: int, op: int = 0):
-    n = lib.mx4_enumerate_tiles(kernel, op, None, 0)
+def mx4_enumerate_tiles(kernel: int, op: int = 0, dtype_code: int = DLA_BF16):
+    n = lib.mx4_enumerate_tiles(kernel, op, dtype_code, None, 0)
     arr = (Mx4Params * n)()
-    lib.mx4_enumerate_tiles(kernel, op, arr, n)
+    lib.mx4_enumerate_tiles(kernel, op, dtype_code, arr, n)
     return [Mx4Params(*a.as_tuple()) for a in arr]
 
 

@@ -150,10 +150,10 @@ int mx4_apply(int op, const void* d_x, int64_t ldx, dla_dtype dt, const void* d_
   return mx4_apply_launch(op, d_x, ldx, dt, m, w, k, d_y, ldy, dt_y, plan, d_workspace, st);
 }
 
-int mx4_enumerate_tiles(int kernel, int op, mx4_params* out, int cap) {
-  if (op != 0 && op != 1) return 0;
+int mx4_enumerate_tiles(int kernel, int op, dla_dtype dt, mx4_params* out, int cap) {
+  if ((op != 0 && op != 1) || !type_size(dt)) return 0;
   if (kernel == DLA_KERNEL_MX4_GEMM) return mx4_gemm_menu(out, cap);
-  if (kernel == DLA_KERNEL_MX4_APPLY) return mx4_apply_menu(op, out, cap);
+  if (kernel == DLA_KERNEL_MX4_APPLY) return mx4_apply_menu(op, dt, out, cap);
   return 0;
 }
 

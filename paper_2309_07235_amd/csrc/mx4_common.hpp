@@ -57,28 +57,6 @@ __device__ __forceinline__ f32x16_t mx_mma32(i32x4_t a, i32x4_t b, f32x16_t c, i
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, OP, sa, OP, sb);
 }
 
-// 16 bytes of every lane from memory (base + off) to LDS without a register in between: lane l's go to byte lds + 16 l; base and
-// lds are the same in all lanes.  Assembly, because the compiler lets every later LDS read wait for all such loads, whatever they
-// write; so the waits are wait_loads_and_barrier's, and nothing else that a kernel's main loop loads may be in flight beside them.
-// There is no register for the load to come back to; the wait state is the one between a write of M0 and its use (nothing else in
-// these kernels uses M0).
-__device__ __forceinline__ void load_to_lds(const void* base, unsigned int off, unsigned int lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
-               : "memory");
-}
-
-// Where an array in LDS starts, for load_to_lds.
-__device__ __forceinline__ unsigned int lds_offset(const void* p) {
-  return __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
-}
-
-// Waits until at most N of the wave's loads are in flight and all its LDS accesses are done, then for the other waves.
-template <int N>
-__device__ __forceinline__ void wait_loads_and_barrier() {
-  static_assert(N < 64, "six bits");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-
 // Eight elements (one dword, low nibble first) times the scale, which is exact in bf16 up to the type's range.
 __device__ __forceinline__ bf16x8_t mx_values(unsigned int w, float scale) {
   union {

@@ -1,7 +1,7 @@
 // C = A*B^T and C += A*B^T with both operands in microscaled 4-bit floating point.
 #pragma once
 #include <type_traits>
-#include "mx4_common.hpp"
+#include "mx4_tile.hpp"
 
 namespace dla {
 
@@ -85,79 +85,6 @@ __global__ void __launch_bounds__(kMxDirectWaves * 64) mx4_gemm_direct_kernel(Mx
       T* const out = static_cast<T*>(g.c) + r * g.ldc + c;
       *out = (T)(g.onto ? (float)*out + sum : sum);
     }
-  }
-}
-
-// Tile `id` of a grid of tiles: eight rows of tiles are walked column by column, so that the workgroups of an XCD, which are
-// neighbours in id, share operands in its L2.
-__device__ __forceinline__ void tile_at(int id, int tiles_m, int tiles_n, int* ti, int* tj) {
-  const int band = 8 * tiles_n, first = id / band * 8, height = min(8, tiles_m - first), in = id % band;
-  *ti = first + in % height;
-  *tj = in / height;
-}
-
-// A wave's part of the result, R x C in 32 x 32 blocks whose lanes hold neighbouring columns, to rows r0.. and columns c0.. of a
-// matrix of `rows` x `cols`; `lds` is the wave's own room, 1024 units of 16 bytes.  It goes through LDS as S, rounded to T (or in
-// fp32 where it is added onto C, which is rounded once), so that rows are written 16 bytes a lane.
-template <int R, int C, typename S, typename T>
-__device__ __forceinline__ void mx_store_tile(u32x4_t* lds, const f32x16_t (&acc)[R / 32][C / 32], int lane, T* c, int64_t ldc, int r0, int c0, int rows,
-                                              int cols, bool onto) {
-  constexpr int PER = 16 / (int)sizeof(S);                              // elements of 16 bytes
-  constexpr int WIDE = C * R * (int)sizeof(S) <= 16384 ? C : 16384 / (R * (int)sizeof(S));  // columns at a time
-  constexpr int CH = WIDE / PER, RPB = CH >= 16 ? 1 : 16 / CH;          // 16-byte chunks of a row; rows of 256 bytes
-  static_assert(WIDE % 32 == 0 && C % WIDE == 0, "whole blocks");
-  typedef S run_t __attribute__((ext_vector_type(PER)));
-  typedef T out_t __attribute__((ext_vector_type(PER)));
-  typedef S quad_t __attribute__((ext_vector_type(4)));
-  const int l31 = lane & 31, l5 = lane >> 5;
-  const bool vec = (uintptr_t)c % sizeof(out_t) == 0 && ldc % PER == 0;
-  // chunk c of a row lies at c ^ (r / RPB) % CH: a wave's accesses take all banks
-  auto place = [&](int r, int chunk) { return r * CH + (chunk ^ ((r / RPB) & (CH - 1))); };
-  auto in_order = [] {  // what other lanes of the wave have written
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  };
-#pragma unroll
-  for (int p = 0; p < C / WIDE; ++p) {
-#pragma unroll
-    for (int i = 0; i < R / 32; ++i)
-#pragma unroll
-      for (int j = 0; j < WIDE / 32; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int col = j * 32 + 8 * q + 4 * l5;
-          quad_t t;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) t[v] = (S)acc[i][p * (WIDE / 32) + j][4 * q + v];
-          reinterpret_cast<quad_t*>(lds + place(i * 32 + l31, col / PER))[col % PER / 4] = t;
-        }
-    in_order();
-    const int first = c0 + p * WIDE;
-#pragma unroll 4
-    for (int e = lane; e < R * CH; e += 64) {
-      const int r = e / CH, chunk = e % CH, row = r0 + r, col = first + chunk * PER;
-      const run_t t = __builtin_bit_cast(run_t, lds[place(r, chunk)]);
-      if (row >= rows || col >= cols) continue;
-      T* const out = c + (int64_t)row * ldc + col;
-      if (vec && col + PER <= cols) {
-        out_t o;
-        if (onto) {
-          o = *reinterpret_cast<const out_t*>(out);
-#pragma unroll
-          for (int v = 0; v < PER; ++v) o[v] = (T)((float)o[v] + (float)t[v]);
-        } else {
-#pragma unroll
-          for (int v = 0; v < PER; ++v) o[v] = (T)t[v];
-        }
-        *reinterpret_cast<out_t*>(out) = o;
-      } else {
-#pragma unroll
-        for (int v = 0; v < PER; ++v)
-          if (col + v < cols) out[v] = (T)(onto ? (float)out[v] + (float)t[v] : (float)t[v]);
-      }
-    }
-    in_order();
   }
 }
 

@@ -23,7 +23,7 @@ int mx4_gemm_plan(int64_t m, int64_t n, int64_t k, const mx4_params* p, MxPlan* 
 int mx4_gemm_launch(bool onto, const Mx4View& a, const Mx4View& b, void* c, int64_t ldc, int64_t k, dla_dtype dt, const MxPlan& plan,
                     float* parts, hipStream_t stream);
 
-int mx4_apply_menu(int op, mx4_params* out, int cap);
+int mx4_apply_menu(int op, dla_dtype dt, mx4_params* out, int cap);
 int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const mx4_params* p, MxPlan* plan);
 int mx4_apply_launch(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, const Mx4View& w, int64_t k, void* y, int64_t ldy,
                      dla_dtype dt_y, const MxPlan& plan, void* workspace, hipStream_t stream);

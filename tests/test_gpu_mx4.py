@@ -233,8 +233,9 @@ def test_gemm_nothing_to_sum_and_empty_results(B):
     assert (f64(y) == 0).all()
 
 
-def apply_params(B, op):
-    return [None] + [B.Mx4Params(t.tile_m, t.tile_n, s) for t in B.mx4_enumerate_tiles(B.DLA_KERNEL_MX4_APPLY, op) for s in (1, 3)]
+def apply_params(B, op, dtype):
+    code = {"float32": B.DLA_F32, "bfloat16": B.DLA_BF16, "float16": B.DLA_F16}[dtype]
+    return [None] + [B.Mx4Params(t.tile_m, t.tile_n, s) for t in B.mx4_enumerate_tiles(B.DLA_KERNEL_MX4_APPLY, op, code) for s in (1, 3)]
 
 
 def legal_apply(B, op, p, terms):
@@ -255,7 +256,7 @@ def test_apply_bit_for_bit(B, dtype, op):
         w = O.values(wc, ws)[:, :k]
         x = rng.integers(-8, 9, (m, k if op == 0 else n)).astype(float)
         exact = x @ (w.T if op == 0 else w)
-        for i, p in enumerate(apply_params(B, op)):
+        for i, p in enumerate(apply_params(B, op, dtype)):
             if not legal_apply(B, op, p, x.shape[1]):
                 continue
             pad = (0, 1, 8)[i % 3]
@@ -281,7 +282,7 @@ def test_apply_against_64_bits(B, dtype, op):
         x = f64(xd)
         w = w.T if op == 0 else w
         want, size = x @ w, np.abs(x) @ np.abs(w)
-        for p in apply_params(B, op):
+        for p in apply_params(B, op, dtype):
             if not legal_apply(B, op, p, x.shape[1]):
                 continue
             announce(f"mx4_apply values op {op} {dtype} {m} x {n} x {k} {p}")
@@ -318,7 +319,7 @@ def test_apply_infinities_nan_and_the_largest_values(B, dtype, op):
     w = O.values(wc, ws)[:, :k]
     with np.errstate(invalid="ignore"):
         want = x @ (w.T if op == 0 else w)
-    for p in apply_params(B, op):
+    for p in apply_params(B, op, dtype):
         if not legal_apply(B, op, p, x.shape[1]):
             continue
         announce(f"mx4_apply special op {op} {dtype} {p}")
@@ -477,12 +478,12 @@ def test_offsets_past_32_bits(B):
         ct = torch.zeros((n, m), device="cuda")
         B.mx4_gemm(0, b, a, ct, p)
         assert np.array_equal(f64(ct), exact.T), p
-    for p in apply_params(B, 0):
+    for p in apply_params(B, 0, "bfloat16"):
         x = rng.integers(-4, 5, (20, k)).astype(float)
         y = torch.zeros((20, m), device="cuda")
         B.mx4_apply(0, put(x, "bfloat16")[1], a, y, p)
         assert np.array_equal(f64(y), x @ O.values(ac, as_)[:, :k].T), p
-    for p in apply_params(B, 1):
+    for p in apply_params(B, 1, "bfloat16"):
         x = rng.integers(-4, 5, (20, m)).astype(float)
         y = torch.zeros((20, k), device="cuda")
         B.mx4_apply(1, put(x, "bfloat16")[1], a, y, p)

@@ -123,7 +123,7 @@ def test_menus_and_default_schedules(B):
                               (5, (kernel, op, 1, 1, 0, 1)), (6, (kernel, op, 1, 1, 1, 0))):
                 assert B.lib.mx4_default_params(*args, r) == -pos
             assert B.lib.mx4_default_params(kernel, op, 1, 1, 1, 1, None) == -7
-    assert B.lib.mx4_enumerate_tiles(0, 0, None, 0) == 0 and B.lib.mx4_enumerate_tiles(3, 2, None, 0) == 0
+    assert B.lib.mx4_enumerate_tiles(0, 0, 1, None, 0) == B.lib.mx4_enumerate_tiles(3, 2, 1, None, 0) == B.lib.mx4_enumerate_tiles(3, 0, 0, None, 0) == 0
     assert [B.lib.mx4_padded(c) for c in (-1, 0, 1, 128, 129)] == [0, 0, 128, 128, 256]
 
 
