@@ -141,7 +141,7 @@ def _load() -> ctypes.CDLL:
     lib.mx4_gemm_workspace_bytes.restype = sz
     lib.mx4_apply.argtypes = [ci, vp, i64, ci, vp, i64, vp, i64, vp, i64, ci, i64, i64, i64, mxp, vp, sz, vp]
     lib.mx4_apply.restype = ci
-    lib.mx4_apply_workspace_bytes.argtypes = [ci, i64, i64, i64, ci, mxp]
+    lib.mx4_apply_workspace_bytes.argtypes = [ci, vp, i64, ci, i64, i64, i64, mxp]
     lib.mx4_apply_workspace_bytes.restype = sz
     lib.mx4_enumerate_tiles.argtypes = [ci, ci, ci, mxp, ci]
     lib.mx4_enumerate_tiles.restype = ci
@@ -397,23 +397,33 @@ def _mx4_dtype(t) -> int:
 
 class Mx4:
     """A microscaled matrix as two uint8 device tensors: q (rows x at least padded / 2) and s (rows x at least padded / 32);
-    see dla.h for their layout.  cols is the number of columns without the padding."""
-    __slots__ = ("q", "s", "cols")
+    see dla.h for their layout.  cols is the number of columns without the padding.  The tensors are looked over once, here: they must
+    not be resized afterwards."""
+    __slots__ = ("q", "s", "rows", "cols", "_device", "_ldq", "_lds")
 
     def __init__(self, q, s, cols: int):
-        self.q, self.s, self.cols = q, s, int(cols)
-
-    @property
-    def rows(self) -> int:
-        return self.q.shape[0]
-
-    def _args(self, name):
-        q, s, wide = self.q, self.s, mx4_padded(self.cols)
+        wide = mx4_padded(cols)
         if q.dim() != 2 or s.dim() != 2 or q.dtype != torch.uint8 or s.dtype != torch.uint8 or s.shape[0] != q.shape[0]:
-            raise ValueError(f"{name}: q and s must be uint8 matrices with the same number of rows")
-        if self.cols < 0 or q.shape[1] * 2 < wide or s.shape[1] * 32 < wide:
-            raise ValueError(f"{name}: q and s must hold {wide} columns (mx4_padded({self.cols}))")
-        return (*_matrix(q, name), *_matrix(s, name))
+            raise ValueError("Mx4: q and s must be uint8 matrices with the same number of rows")
+        if cols < 0 or q.shape[1] * 2 < wide or s.shape[1] * 32 < wide:
+            raise ValueError(f"Mx4: q and s must hold {wide} columns (mx4_padded({cols}))")
+        if s.device != q.device:
+            raise ValueError("Mx4: q and s on different devices")
+        self.q, self.s, self.rows, self.cols, self._device = q, s, q.shape[0], int(cols), q.get_device()
+        self._ldq, self._lds = _leading(q, "q"), _leading(s, "s")
+
+    def _args(self):
+        return self.q.data_ptr() or None, self._ldq, self.s.data_ptr() or None, self._lds
+
+
+def _leading(t, name: str) -> int:
+    """The leading dimension of a row-major matrix."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    (rows, cols), (row, col) = t.shape, t.stride()
+    if col != 1 and cols > 1:
+        raise ValueError(f"{name} must be a row-major matrix (unit column stride)")
+    return (row if rows > 1 else cols) or 1
 
 
 def mx4_padded(cols: int) -> int:
@@ -428,69 +438,74 @@ def mx4_empty(rows: int, cols: int, device="cuda") -> Mx4:
                torch.empty((rows, wide // 32), dtype=torch.uint8, device=device), cols)
 
 
-def _mx4_call(fn, name, stream, tensors, args):
-    """fn(*args, stream) on the device that holds the tensors."""
-    device = tensors[0].device
-    for t in tensors:
-        if t.device != device:
-            raise ValueError(f"{name}: tensors on different devices")
-    if device.type != "cuda":
+def _mx4_call(fn, name: str, stream, devices, args):
+    """fn(*args, stream) on the one device of `devices` (indices, -1: host memory)."""
+    device = devices[0]
+    if device < 0:
         raise ValueError(f"{name}: tensors must live in device memory")
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, _stream_ptr(stream))
+    for d in devices:
+        if d != device:
+            raise ValueError(f"{name}: tensors on different devices")
+    # (the raw stream: torch.cuda.current_stream() takes 3 us to make an object of it, as long as the call itself)
+    raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+    if device == torch.cuda.current_device():
+        rc = fn(*args, raw)
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, _stream_ptr(stream))
-    _check(rc, name)
+            rc = fn(*args, raw)
+    if rc != DLA_SUCCESS:
+        raise DlaError(rc, name)
 
 
 def mx4_quantize(x, q: Mx4 | None = None, qt: Mx4 | None = None, stream=None):
     """The microscaled form of the device matrix x into q, of its transpose into qt; either may be None (see dla.h: mx4_quantize)."""
     if q is None and qt is None:
         raise ValueError("mx4_quantize: neither q nor qt")
-    xp, ldx = _matrix(x, "x")
+    ldx = _leading(x, "x")
     rows, cols = x.shape
-    tensors, args = [x], [xp, ldx, rows, cols, _mx4_dtype(x)]
-    for name, form, want in (("q", q, (rows, cols)), ("qt", qt, (cols, rows))):
+    devices, args = [x.get_device()], [x.data_ptr() or None, ldx, rows, cols, _mx4_dtype(x)]
+    for form, r, c in ((q, rows, cols), (qt, cols, rows)):
         if form is None:
-            args += [None, 0, None, 0]
+            args += (None, 0, None, 0)
             continue
-        if (form.rows, form.cols) != want:
-            raise ValueError(f"mx4_quantize: {name} must be {want[0]} x {want[1]}")
-        args += form._args(name)
-        tensors += [form.q, form.s]
-    _mx4_call(lib.mx4_quantize, "mx4_quantize", stream, tensors, args)
+        if form.rows != r or form.cols != c:
+            raise ValueError(f"mx4_quantize: {'q' if form is q else 'qt'} must be {r} x {c}")
+        args += form._args()
+        devices.append(form._device)
+    _mx4_call(lib.mx4_quantize, "mx4_quantize", stream, devices, args)
 
 
 def mx4_dequantize(q: Mx4, y, stream=None):
     """y = the values of q, rounded to y's type (see dla.h: mx4_dequantize)."""
-    if tuple(y.shape) != (q.rows, q.cols):
+    ldy = _leading(y, "y")
+    if y.shape[0] != q.rows or y.shape[1] != q.cols:
         raise ValueError("mx4_dequantize: q and y differ in shape")
-    _mx4_call(lib.mx4_dequantize, "mx4_dequantize", stream, (q.q, q.s, y),
-              (*q._args("q"), q.rows, q.cols, _mx4_dtype(y), *_matrix(y, "y")))
+    _mx4_call(lib.mx4_dequantize, "mx4_dequantize", stream, (q._device, y.get_device()),
+              (*q._args(), q.rows, q.cols, _mx4_dtype(y), y.data_ptr() or None, ldy))
 
 
 def _mx4_workspace(need: int, device, workspace, stream):
+    """The workspace, its address, its bytes and its device's index."""
     if workspace is None:
         if not need:
-            return None, None, 0
+            return None, None, 0, None
         with torch.cuda.stream(stream):  # memory of the stream that uses it (None: the current one)
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace.get_device()
 
 
 def mx4_gemm(op: int, a: Mx4, b: Mx4, c, p: Mx4Params | None = None, workspace=None, stream=None):
     """c = a*b^T (op 0) or c += a*b^T (op 1), both operands microscaled (see dla.h: mx4_gemm).  Returns the workspace it used
     (None where the schedule needs none)."""
-    m, n, k = a.rows, b.rows, a.cols
-    if b.cols != k or tuple(c.shape) != (m, n):
+    m, n, k, ldc = a.rows, b.rows, a.cols, _leading(c, "c")
+    if b.cols != k or c.shape[0] != m or c.shape[1] != n:
         raise ValueError("mx4_gemm: shapes do not chain")
-    pr = _ref(p)
+    pr, dt = _ref(p), _mx4_dtype(c)
     need = lib.mx4_gemm_workspace_bytes(m, n, k, pr) if workspace is None else 0
-    ws, wsp, wsb = _mx4_workspace(need, c.device, workspace, stream)
-    tensors = (c, a.q, a.s, b.q, b.s) if ws is None else (c, a.q, a.s, b.q, b.s, ws)
-    _mx4_call(lib.mx4_gemm, "mx4_gemm", stream, tensors,
-              (op, *a._args("a"), *b._args("b"), *_matrix(c, "c"), m, n, k, _mx4_dtype(c), pr, wsp, wsb))
+    ws, wsp, wsb, wsd = _mx4_workspace(need, c.device, workspace, stream)
+    devices = (c.get_device(), a._device, b._device) if ws is None else (c.get_device(), a._device, b._device, wsd)
+    _mx4_call(lib.mx4_gemm, "mx4_gemm", stream, devices,
+              (op, *a._args(), *b._args(), c.data_ptr() or None, ldc, m, n, k, dt, pr, wsp, wsb))
     return ws
 
 
@@ -499,16 +514,17 @@ def mx4_apply(op: int, x, w: Mx4, y, p: Mx4Params | None = None, workspace=None,
     the schedule needs none)."""
     if op not in (0, 1):
         raise ValueError("mx4_apply: op must be 0 or 1")
+    ldx, ldy = _leading(x, "x"), _leading(y, "y")
     m, n, k = x.shape[0], w.rows, w.cols
     terms, out = (k, n) if op == 0 else (n, k)
-    if x.dim() != 2 or x.shape[1] != terms or tuple(y.shape) != (m, out):
+    if x.shape[1] != terms or y.shape[0] != m or y.shape[1] != out:
         raise ValueError("mx4_apply: shapes do not chain")
-    pr, dt = _ref(p), _mx4_dtype(x)
-    need = lib.mx4_apply_workspace_bytes(op, m, n, k, dt, pr) if workspace is None else 0
-    ws, wsp, wsb = _mx4_workspace(need, y.device, workspace, stream)
-    tensors = (x, w.q, w.s, y) if ws is None else (x, w.q, w.s, y, ws)
-    _mx4_call(lib.mx4_apply, "mx4_apply", stream, tensors,
-              (op, *_matrix(x, "x"), dt, *w._args("w"), *_matrix(y, "y"), _mx4_dtype(y), m, n, k, pr, wsp, wsb))
+    pr, dt, dty, xp = _ref(p), _mx4_dtype(x), _mx4_dtype(y), x.data_ptr() or None
+    need = lib.mx4_apply_workspace_bytes(op, xp, ldx, dt, m, n, k, pr) if workspace is None else 0
+    ws, wsp, wsb, wsd = _mx4_workspace(need, y.device, workspace, stream)
+    devices = (x.get_device(), w._device, y.get_device()) if ws is None else (x.get_device(), w._device, y.get_device(), wsd)
+    _mx4_call(lib.mx4_apply, "mx4_apply", stream, devices,
+              (op, xp, ldx, dt, *w._args(), y.data_ptr() or None, ldy, dty, m, n, k, pr, wsp, wsb))
     return ws
 
 

@@ -108,11 +108,11 @@ int mx4_gemm(int op, const void* d_a, int64_t lda, const void* d_sa, int64_t lds
   return mx4_gemm_launch(op == 1, a, b, d_c, ldc, k, dt, plan, (float*)d_workspace, st);
 }
 
-size_t mx4_apply_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const mx4_params* p) {
+size_t mx4_apply_workspace_bytes(int op, const void* d_x, int64_t ldx, dla_dtype dt, int64_t m, int64_t n, int64_t k, const mx4_params* p) {
   MxPlan plan;
   if ((op != 0 && op != 1) || m <= 0 || n <= 0 || k <= 0 || m > kMaxDim || n > kMaxDim || k > kMaxDim || !type_size(dt)) return 0;
   if (mx4_apply_plan(op, m, n, k, dt, p, &plan) != DLA_SUCCESS) return 0;
-  return mx4_apply_bytes(op, m, n, k, dt, plan);
+  return mx4_apply_bytes(op, d_x, ldx, dt, m, n, k, plan);
 }
 
 int mx4_apply(int op, const void* d_x, int64_t ldx, dla_dtype dt, const void* d_w, int64_t ldw, const void* d_sw, int64_t ldsw,
@@ -142,7 +142,7 @@ int mx4_apply(int op, const void* d_x, int64_t ldx, dla_dtype dt, const void* d_
     hip_clear_stale_error();
     return mx4_fill_zero_launch(d_y, ldy, m, out, dt_y, st);
   }
-  const size_t need = mx4_apply_bytes(op, m, n, k, dt, plan);
+  const size_t need = mx4_apply_bytes(op, d_x, ldx, dt, m, n, k, plan);
   if (need && (!d_workspace || (uintptr_t)d_workspace % 256 || workspace_bytes < need)) return DLA_ERR_WORKSPACE;
   hip_clear_stale_error();
   const Mx4View w = {(const uint8_t*)d_w, (const uint8_t*)d_sw, ldw, ldsw, (int)n};

@@ -6,14 +6,17 @@ namespace dla {
 namespace {
 
 constexpr int kMaxSplits = 32;
-constexpr int kDirect = 16;  // the tile of the direct kernels
+constexpr int kDirect = 32;  // columns of a direct kernel's tile
 
 struct Tile {
   int m, n;
 };
-const Tile kTiles[] = {{kDirect, kDirect}, {128, 128}, {256, 256}};
+const Tile kTiles[] = {{16, kDirect}, {32, kDirect}, {48, kDirect}, {64, kDirect}, {128, 128}, {256, 256}};
 
-bool legal(const Tile& t, dla_dtype dt) { return t.m < 256 || dt == DLA_BF16; }  // two or three terms of 256 rows do not fit the LDS
+// The direct kernels are for op 0; more than 32 rows of fp32, or two or three terms of 256 rows, do not fit the LDS.
+bool legal(const Tile& t, int op, dla_dtype dt) {
+  return t.n == kDirect ? op == 0 && (t.m <= 32 || dt != DLA_F32) : t.m < 256 || dt == DLA_BF16;
+}
 
 int64_t wide(int64_t terms) { return (terms + 63) / 64 * 64; }
 
@@ -22,20 +25,46 @@ bool whole(const void* x, int64_t ldx, dla_dtype dt, int64_t terms) {
   return dt == DLA_BF16 && (uintptr_t)x % 16 == 0 && ldx % 8 == 0 && terms % 64 == 0 && ldx <= kMxMaxLd / 2;
 }
 
-size_t planes_bytes(int64_t m, int64_t terms, dla_dtype dt) {
-  const int64_t count = dt == DLA_F32 ? 3 : dt == DLA_F16 ? 2 : 1;
-  return ((size_t)(count * m * wide(terms)) * 2 + 255) / 256 * 256;
+// X as the direct kernel takes it: aligned rows of whole steps (and offsets inside a tile of 64 rows in 32 bits).
+bool direct_takes(const void* x, int64_t ldx, int size, int64_t terms) {
+  return (uintptr_t)x % 16 == 0 && ldx * size % 16 == 0 && terms % kMxStep == 0 && ldx * size <= (int64_t)1 << 25;
 }
 
-template <dla_dtype DT, typename TY>
-int launch_direct(int op, const MxApplyArgs& g, hipStream_t stream) {
-  using T = typename MxType<DT>::type;
-  constexpr int TERMS = MxType<DT>::kTerms;
-  const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * g.splits));
-  if (op == 0)
-    hipLaunchKernelGGL((mx4_apply_direct_kernel<T, TERMS, TY>), grid, dim3(kMxApplyWaves * 64), 0, stream, g);
-  else
-    hipLaunchKernelGGL((mx4_apply_grad_direct_kernel<T, TERMS, TY>), grid, dim3(64), 0, stream, g);
+// The room for what a kernel reads instead of X.
+size_t copy_bytes(const MxPlan& plan, int64_t m, int64_t terms, dla_dtype dt) {
+  const int64_t count = plan.tile_n == kDirect ? (terms + kMxStep - 1) / kMxStep * kMxStep * (dt == DLA_F32 ? 4 : 2)
+                                               : wide(terms) * 2 * (dt == DLA_F32 ? 3 : dt == DLA_F16 ? 2 : 1);
+  return ((size_t)(m * count) + 255) / 256 * 256;
+}
+
+template <typename T, int MB, int XI, int WV, int DW>
+int launch_direct_as(const MxApplyArgs& g, hipStream_t stream) {
+  hipLaunchKernelGGL((mx4_apply_direct_kernel<T, MB, XI, WV, DW>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(WV * 64), 0, stream, g);
+  return launch_status(__func__);
+}
+
+// How many waves and how far ahead is what the LDS holds.  One load of X takes four rows of 16-bit elements or two of fp32.
+template <typename T>
+int launch_direct(const MxApplyArgs& g, int tile_m, hipStream_t stream) {
+  constexpr bool wide_t = sizeof(T) == 4;
+  switch (tile_m) {
+    case 16:
+      if (g.m <= (wide_t ? 2 : 4)) return launch_direct_as<T, 1, 1, wide_t ? 4 : 8, 4>(g, stream);
+      return launch_direct_as<T, 1, wide_t ? 8 : 4, wide_t ? 4 : 8, 4>(g, stream);
+    case 32: return launch_direct_as<T, 2, wide_t ? 16 : 8, 4, wide_t ? 3 : 6>(g, stream);
+  }
+  if constexpr (!wide_t) {
+    if (tile_m == 48) return launch_direct_as<T, 3, 12, 4, 6>(g, stream);
+    if (tile_m == 64) return launch_direct_as<T, 4, 16, 4, 3>(g, stream);
+  }
+  return DLA_ERR_UNSUPPORTED_PARAMS;
+}
+
+template <typename T>
+int launch_copy(const T* x, int64_t ldx, int64_t m, int64_t terms, int64_t to_ld, T* to, hipStream_t stream) {
+  const int64_t per_row = to_ld / 8, groups = (m * per_row + 255) / 256;
+  if (groups > 0x7fffffff) return DLA_ERR_TOO_LARGE;
+  hipLaunchKernelGGL(mx4_copy_kernel<T>, dim3((unsigned)groups), dim3(256), 0, stream, x, ldx, m, terms, (int)per_row, to);
   return launch_status(__func__);
 }
 
@@ -66,11 +95,6 @@ int launch_typed(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w
   const int64_t out = op == 0 ? w.rows : k, terms = op == 0 ? k : w.rows;
   const int tiles_m = (int)((m + plan.tile_m - 1) / plan.tile_m), tiles_n = (int)((out + plan.tile_n - 1) / plan.tile_n);
   float* const parts = static_cast<float*>(workspace);
-  if (plan.tile_m == kDirect) {
-    const bool vec = (uintptr_t)x % 16 == 0 && ldx * (int64_t)sizeof(typename MxType<DT>::type) % 16 == 0;
-    const MxApplyArgs g = {x, w, y, parts, ldx, ldy, (int)m, w.rows, (int)k, plan.splits, tiles_m, tiles_n, vec};
-    return launch_direct<DT, TY>(op, g, stream);
-  }
   MxApplyTileArgs g = {static_cast<const __bf16*>(x), w, y, parts, ldx, 0, ldy, (int)m, (int)out, (int)((k + kMxStep - 1) / kMxStep * kMxStep),
                        (int)(wide(terms) / 64), plan.splits, tiles_m, tiles_n};
   if (!whole(x, ldx, DT, terms)) {
@@ -90,6 +114,20 @@ int launch_typed(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w
 template <dla_dtype DT>
 int launch_to(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w, int64_t k, void* y, int64_t ldy, dla_dtype dt_y, const MxPlan& plan,
               void* workspace, hipStream_t stream) {
+  using T = typename MxType<DT>::type;
+  if (plan.tile_n == kDirect) {
+    const int64_t steps = (k + kMxStep - 1) / kMxStep;
+    MxApplyArgs g = {x, w, y, static_cast<float*>(workspace), ldx, ldy, (int)m, (int)steps, plan.splits, (int)((m + plan.tile_m - 1) / plan.tile_m),
+                     (w.rows + kDirect - 1) / kDirect, dt_y};
+    if (!direct_takes(x, ldx, sizeof(T), k)) {
+      T* const to = reinterpret_cast<T*>(static_cast<char*>(workspace) + mx4_parts_bytes(m, w.rows, plan));
+      const int rc = launch_copy<T>(static_cast<const T*>(x), ldx, m, k, steps * kMxStep, to, stream);
+      if (rc != DLA_SUCCESS) return rc;
+      g.x = to;
+      g.ldx = steps * kMxStep;
+    }
+    return launch_direct<T>(g, plan.tile_m, stream);
+  }
   if (dt_y == DLA_F32) return launch_typed<DT, float>(op, x, ldx, m, w, k, y, ldy, plan, workspace, stream);
   if (dt_y == DLA_BF16) return launch_typed<DT, __bf16>(op, x, ldx, m, w, k, y, ldy, plan, workspace, stream);
   return launch_typed<DT, _Float16>(op, x, ldx, m, w, k, y, ldy, plan, workspace, stream);
@@ -97,10 +135,10 @@ int launch_to(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w, i
 
 }  // namespace
 
-int mx4_apply_menu(int, dla_dtype dt, mx4_params* out, int cap) {
+int mx4_apply_menu(int op, dla_dtype dt, mx4_params* out, int cap) {
   int count = 0;
   for (const Tile& t : kTiles) {
-    if (!legal(t, dt)) continue;
+    if (!legal(t, op, dt)) continue;
     if (out && count < cap) out[count] = mx4_params{t.m, t.n, 0};
     ++count;
   }
@@ -112,9 +150,13 @@ int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const 
   if (p) r = MxPlan{p->tile_m, p->tile_n, p->splits};
   const int64_t terms = op == 0 ? k : n, out = op == 0 ? n : k;
   if (r.tile_m < 0 || r.tile_n < 0 || r.splits < 0 || r.splits > kMaxSplits || r.splits > (terms + kMxStep - 1) / kMxStep) return DLA_ERR_UNSUPPORTED_PARAMS;
-  if (r.tile_m == 0 && r.tile_n == 0) r.tile_m = r.tile_n = m <= 32 ? 16 : (m < 1024 || dt != DLA_BF16) ? 128 : 256;
+  if (r.tile_m == 0 && r.tile_n == 0) {
+    const bool direct = op == 0 && m <= (dt == DLA_F32 ? 32 : 64);
+    r.tile_m = direct ? (int)(m + 15) / 16 * 16 : m < 1024 || dt != DLA_BF16 ? 128 : 256;
+    r.tile_n = direct ? kDirect : r.tile_m;
+  }
   bool found = false;
-  for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n && legal(t, dt);
+  for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n && legal(t, op, dt);
   if (!found) return DLA_ERR_UNSUPPORTED_PARAMS;
   if (r.splits == 0) r.splits = 1;
   const int64_t tiles = ((m + r.tile_m - 1) / r.tile_m) * ((out + r.tile_n - 1) / r.tile_n);
@@ -123,8 +165,10 @@ int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const 
   return DLA_SUCCESS;
 }
 
-size_t mx4_apply_bytes(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const MxPlan& plan) {
-  return mx4_parts_bytes(m, op == 0 ? n : k, plan) + (plan.tile_m == kDirect ? 0 : planes_bytes(m, op == 0 ? k : n, dt));
+size_t mx4_apply_bytes(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, int64_t n, int64_t k, const MxPlan& plan) {
+  const int64_t terms = op == 0 ? k : n;
+  const bool as_it_is = plan.tile_n == kDirect ? direct_takes(x, ldx, dt == DLA_F32 ? 4 : 2, terms) : whole(x, ldx, dt, terms);
+  return mx4_parts_bytes(m, op == 0 ? n : k, plan) + (as_it_is ? 0 : copy_bytes(plan, m, terms, dt));
 }
 
 int mx4_apply_launch(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, const Mx4View& w, int64_t k, void* y, int64_t ldy, dla_dtype dt_y,

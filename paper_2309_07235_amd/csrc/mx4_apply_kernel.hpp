@@ -1,38 +1,31 @@
 // Y = X*W^T and Y = X*W with W in microscaled 4-bit floating point and X in ordinary floating point.
 #pragma once
+#include <type_traits>
 #include "mx4_tile.hpp"
 
 namespace dla {
 
 struct MxApplyArgs {
-  const void* x;
+  const void* x;         // rows aligned to 16 bytes, whole steps of 128 terms
   Mx4View w;
   void* y;
   float* parts;
   int64_t ldx, ldy;
-  int m, n, k;  // X m x k and Y m x n for op 0, X m x n and Y m x k for op 1; W n x k
+  int m, steps;          // Y m x w.rows, steps of 128 terms
   int splits, tiles_m, tiles_n;
-  bool vec;     // rows of X are aligned to 16 bytes
+  dla_dtype dt_y;
 };
 
-// Eight elements of X as bf16 terms, those from `valid` on zero.
+// Eight elements of X as bf16 terms.
 template <typename T, int TERMS>
-__device__ __forceinline__ void mx_load_terms(const T* p, int valid, bool vec, bf16x8_t* t) {
-  typedef T run_t __attribute__((ext_vector_type(8)));
-  union {
-    unsigned short u[8];
-    bf16x8_t v;
-  } o[TERMS];
-  run_t r;
-  if (vec && valid >= 8) {
-    r = *reinterpret_cast<const run_t*>(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = i < valid ? p[i] : (T)0.0f;
-  }
+__device__ __forceinline__ void mx_terms_of(T __attribute__((ext_vector_type(8))) r, bf16x8_t* t) {
   if constexpr (TERMS == 1) {
-    o[0].v = r;
+    t[0] = r;
   } else {
+    union {
+      unsigned short u[8];
+      bf16x8_t v;
+    } o[TERMS];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       unsigned short s[TERMS];
@@ -40,59 +33,223 @@ __device__ __forceinline__ void mx_load_terms(const T* p, int valid, bool vec, b
 #pragma unroll
       for (int j = 0; j < TERMS; ++j) o[j].u[i] = s[j];
     }
-  }
 #pragma unroll
-  for (int j = 0; j < TERMS; ++j) t[j] = o[j].v;
+    for (int j = 0; j < TERMS; ++j) t[j] = o[j].v;
+  }
 }
 
-constexpr int kMxApplyWaves = 8;
+// Few rows of X: what bounds the call is reading W once.  The WV waves of a workgroup share the sum over k, each with a run of
+// steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X two.  Through LDS, because the matrix instructions
+// want neighbouring lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16 (4096 x 16384 weights,
+// one row, bf16: 16 us with loads to registers).
+//   bf16, fp32   a lane's block of W is made bf16 with its scale, X is one or three terms; instruction b takes eight elements of
+//                every lane's block;
+//   fp16         lanes exchange dwords so that instruction b takes block b, whose elements are made fp16 without the scale (with it
+//                they would leave the type's range); the sum is scaled on its way to the running one, in fp32.
+// XI: loads of X a step, fewer than its MB * 16 rows would take where only the first rows exist; what the others hold in LDS reaches rows
+// of the result that are not stored.
+template <typename T>
+struct MxOperand {
+  static constexpr int kTerms = 3;
+  typedef bf16x8_t type;
+};
+template <>
+struct MxOperand<__bf16> {
+  static constexpr int kTerms = 1;
+  typedef bf16x8_t type;
+};
+template <>
+struct MxOperand<_Float16> {
+  static constexpr int kTerms = 1;
+  typedef f16x8_t type;
+};
 
-// Few rows: operands go from memory to the matrix instructions, the eight waves of a workgroup share the sum.  A lane holds 32
-// neighbouring elements of a row of W, one block; instruction j of a step of 128 takes its elements 8j .. 8j + 7, and X's likewise.
-template <typename T, int TERMS, typename TY>
-__global__ void __launch_bounds__(kMxApplyWaves * 64) mx4_apply_direct_kernel(MxApplyArgs g) {
-  constexpr int TM = 16, TN = 16;
-  __shared__ float part[kMxApplyWaves][TM * TN];
+template <typename T, int MB, int XI, int WV, int DW>
+__global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g) {
+  constexpr int NB = 2, TM = MB * 16, TN = NB * 16, TERMS = MxOperand<T>::kTerms;
+  constexpr bool F16 = std::is_same<T, _Float16>::value;
+  constexpr int XCH = kMxStep * (int)sizeof(T) / 16, RPI = 64 / XCH;   // 16-byte chunks of a row and step; rows a load fills
+  constexpr int PER = 8 * (int)sizeof(T) / 16;                         // chunks of eight elements
+  constexpr int W_RING = DW * NB * 64, X_STAGE = TM * XCH, RING = W_RING + 2 * X_STAGE + 2 * TN;  // units of 16 bytes
+  static_assert(WV * RING * 16 <= 160 * 1024 && RING * 16 >= TM * TN * 4, "LDS");
+  using V = typename MxOperand<T>::type;
+  typedef T run_t __attribute__((ext_vector_type(8)));
+  __shared__ u32x4_t lds[WV * RING];
   const int tiles = g.tiles_m * g.tiles_n;
   const int split = (int)blockIdx.x / tiles, tile = (int)blockIdx.x % tiles;
   const int m0 = tile % g.tiles_m * TM, n0 = tile / g.tiles_m * TN;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l15 = lane & 15, l4 = lane >> 4;
-  const int steps = (g.k + kMxStep - 1) / kMxStep;
-  const int share = split * kMxApplyWaves + wave, shares = g.splits * kMxApplyWaves;
-  const int begin = (int)((int64_t)steps * share / shares), end = (int)((int64_t)steps * (share + 1) / shares);
-  const T* const x = static_cast<const T*>(g.x) + (int64_t)min(m0 + l15, g.m - 1) * g.ldx + l4 * 32;
-  const int64_t row = min(n0 + l15, g.n - 1);
-  const uint8_t* const wq = g.w.q + row * g.w.ldq + l4 * 16;
-  const uint8_t* const ws = g.w.s + row * g.w.lds + l4;
-  float4_t acc = {0, 0, 0, 0};
-  for (int s = begin; s < end; ++s) {
-    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(wq + (int64_t)s * 64);
-    const float sc = mx_scale(ws[(int64_t)s * 4]);
-    const int left = g.k - s * kMxStep - l4 * 32;
+  const int share = split * WV + wave, shares = g.splits * WV;
+  const int begin = (int)((int64_t)g.steps * share / shares), end = (int)((int64_t)g.steps * (share + 1) / shares);
+  u32x4_t* const ring = lds + wave * RING;
+  const unsigned int at_w = lds_offset(ring), at_x = at_w + W_RING * 16, at_s = at_x + 2 * X_STAGE * 16;
+
+  // W: a load fills 16 rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4; X: RPI rows, chunk c of row r at c ^ r % 16
+  const uint8_t* const wq = g.w.q + (int64_t)n0 * g.w.ldq;
+  const uint8_t* const ws = g.w.s + (int64_t)n0 * g.w.lds;
+  const T* const x = static_cast<const T*>(g.x) + (int64_t)m0 * g.ldx;
+  unsigned int woff[NB], xoff[XI];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bf16x8_t t[TERMS];
-      mx_load_terms<T, TERMS>(x + (int64_t)s * kMxStep + 8 * j, left - 8 * j, g.vec, t);
-      const bf16x8_t b = mx_values(w[j], sc);
+  for (int j = 0; j < NB; ++j)
+    woff[j] = (unsigned int)(min(j * 16 + lane / 4, g.w.rows - 1 - n0) * (int)g.w.ldq) + ((lane & 3) ^ (lane >> 4)) * 16;
 #pragma unroll
-      for (int i = TERMS - 1; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[i], b, acc, 0, 0, 0);
+  for (int i = 0; i < XI; ++i) {
+    const int r = i * RPI + lane / XCH;
+    xoff[i] = (unsigned int)min(r, g.m - 1 - m0) * (unsigned int)(g.ldx * (int)sizeof(T)) + ((lane % XCH) ^ (r & 15)) * 16;
+  }
+  const unsigned int soff = (unsigned int)(min(lane & 31, g.w.rows - 1 - n0) * (int)g.w.lds);
+  // (loads past the end repeat its last step, so that their number in flight is always the same)
+  auto load_w = [&](int s, int slot) {
+    const int64_t from = (int64_t)min(s, end - 1) * 64;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) load_to_lds(wq + from, woff[j], at_w + (slot * NB + j) * 1024);
+  };
+  auto load_x = [&](int s, int slot) {
+    const T* const from = x + (int64_t)min(s, end - 1) * kMxStep;
+#pragma unroll
+    for (int i = 0; i < XI; ++i) load_to_lds(from, xoff[i], at_x + slot * X_STAGE * 16 + i * 1024);
+  };
+  // the scales of four steps, 16 bytes a row, moved back to begin at most four steps before the row's end
+  auto scales_from = [&](int chunk) { return min(begin + chunk * 4, g.steps - 4); };
+  auto load_s = [&](int chunk) {
+    if (lane < TN) load_to_lds(ws + (int64_t)scales_from(chunk) * 4, soff, at_s + (chunk & 1) * TN * 16);
+  };
+
+  float4_t acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
+
+  if (begin < end) {
+    if (g.steps >= 4) {
+      load_s(0);
+    } else if (lane < TN) {
+      u32x4_t w = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (begin + i < end) w[i] = *reinterpret_cast<const unsigned int*>(ws + soff + (begin + i) * 4);
+      ring[W_RING + 2 * X_STAGE + lane] = w;
+    }
+#pragma unroll
+    for (int i = 0; i < DW; ++i) {
+      load_w(begin + i, i);
+      if (i >= DW - 2) load_x(begin + i - (DW - 2), i - (DW - 2));
+    }
+    int slot = 0;
+    for (int s = begin; s < end; ++s) {
+      const int i = s - begin, chunk = i >> 2;
+      wait_loads<NB + XI>();  // this step has arrived: only the next one's loads of X, and W's beside them, are younger
+      const u32x4_t* const wr = ring + slot * NB * 64;
+      const u32x4_t* const xr = ring + W_RING + (i & 1) * X_STAGE;
+      const unsigned int* const sr = reinterpret_cast<const unsigned int*>(ring + W_RING + 2 * X_STAGE + (chunk & 1) * TN) + (g.steps >= 4 ? s - scales_from(chunk) : i);
+      unsigned int w[NB][4], sc[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const u32x4_t q = wr[j * 64 + l15 * 4 + (l4 ^ (l15 >> 2))];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) w[j][b] = q[b];
+        sc[j] = sr[(j * 16 + l15) * 4];
+      }
+      run_t xv[4][MB];
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int k = 0; k < MB; ++k) {
+          const int r = k * 16 + l15, c = (F16 ? b * 4 + l4 : l4 * 4 + b) * PER;
+          union {
+            u32x4_t u[PER];
+            run_t v;
+          } o;
+#pragma unroll
+          for (int p = 0; p < PER; ++p) o.u[p] = xr[r * XCH + ((c + p) ^ l15)];
+          xv[b][k] = o.v;
+        }
+      wait_lds();  // (before what was read is overwritten)
+      if ((i & 3) == 0 && s + 4 < end) load_s(chunk + 1);
+      load_w(s + DW, slot);
+      load_x(s + 2, i & 1);
+      slot = slot + 1 == DW ? 0 : slot + 1;
+
+      float own[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if constexpr (F16) {
+          swap_halves(w[j][0], w[j][2]);
+          swap_halves(w[j][1], w[j][3]);
+          swap_rows(w[j][0], w[j][1]);
+          swap_rows(w[j][2], w[j][3]);
+        } else {
+          own[j] = mx_scale(sc[j] >> (8 * l4));
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        V xt[MB][TERMS];
+#pragma unroll
+        for (int k = 0; k < MB; ++k) {
+          if constexpr (F16)
+            xt[k][0] = xv[b][k];
+          else
+            mx_terms_of<T, TERMS>(xv[b][k], xt[k]);
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          if constexpr (F16) {
+            const V wv = mx_values_f16(w[j][b]);
+            const float f = mx_scale_value(sc[j] >> (8 * b));
+#pragma unroll
+            for (int k = 0; k < MB; ++k) {
+              const float4_t sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(xt[k][0], wv, float4_t{0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+              for (int v = 0; v < 4; ++v) acc[k][j][v] = __builtin_fmaf(sum[v], f, acc[k][j][v]);
+            }
+          } else {
+            const V wv = mx_values(w[j][b], own[j]);
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t)
+#pragma unroll
+              for (int k = 0; k < MB; ++k) acc[k][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt[k][t], wv, acc[k][j], 0, 0, 0);
+          }
+        }
+      }
     }
   }
+  wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
+  float* const part = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int v = 0; v < 4; ++v) part[wave][(l4 * 4 + v) * TN + l15] = acc[v];
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) part[wave * TM * TN + (i * 16 + l4 * 4 + v) * TN + j * 16 + l15] = acc[i][j][v];
   __syncthreads();
-  for (int e = threadIdx.x; e < TM * TN; e += kMxApplyWaves * 64) {
+  for (int e = threadIdx.x; e < TM * TN; e += WV * 64) {
     const int r = m0 + e / TN, c = n0 + e % TN;
-    if (r >= g.m || c >= g.n) continue;
+    if (r >= g.m || c >= g.w.rows) continue;
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kMxApplyWaves; ++w) sum += part[w][e];
+    for (int w = 0; w < WV; ++w) sum += part[w * TM * TN + e];
     if (g.splits > 1)
-      g.parts[((int64_t)split * g.m + r) * g.n + c] = sum;
+      g.parts[((int64_t)split * g.m + r) * g.w.rows + c] = sum;
     else
-      static_cast<TY*>(g.y)[r * g.ldy + c] = (TY)sum;
+      store_value(g.y, (int64_t)r * g.ldy + c, sum, g.dt_y, false);
   }
+}
+
+// X in aligned rows of `per_row` runs of eight, zeros behind its columns: what the direct kernel reads where X's own are not so.
+template <typename T>
+__global__ void __launch_bounds__(256) mx4_copy_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int per_row, T* to) {
+  typedef T run_t __attribute__((ext_vector_type(8)));
+  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
+  const unsigned int at = (unsigned int)(first - row0 * per_row) + threadIdx.x;
+  const int64_t row = row0 + at / (unsigned int)per_row, chunk = at % (unsigned int)per_row;
+  if (row >= rows) return;
+  run_t r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = chunk * 8 + i < cols ? x[row * ldx + chunk * 8 + i] : (T)0.0f;
+  *reinterpret_cast<run_t*>(to + (row * per_row + chunk) * 8) = r;
 }
 
 // X as TERMS planes of bf16 that add up to it, rows of `wide` (a multiple of 64) with zeros behind `cols`: what the tile kernel
@@ -103,9 +260,18 @@ __global__ void __launch_bounds__(256) mx4_planes_kernel(const T* x, int64_t ldx
   const unsigned int at = (unsigned int)(first - row0 * per_row) + threadIdx.x;
   const int64_t row = row0 + at / (unsigned int)per_row, chunk = at % (unsigned int)per_row;
   if (row >= rows) return;
-  bf16x8_t t[TERMS];
+  typedef T run_t __attribute__((ext_vector_type(8)));
+  const T* const p = x + row * ldx + chunk * 8;
   const int64_t left = cols - chunk * 8;
-  mx_load_terms<T, TERMS>(x + row * ldx + chunk * 8, left > 8 ? 8 : (int)left, vec, t);
+  run_t r;
+  if (vec && left >= 8) {
+    r = *reinterpret_cast<const run_t*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = i < left ? p[i] : (T)0.0f;
+  }
+  bf16x8_t t[TERMS];
+  mx_terms_of<T, TERMS>(r, t);
 #pragma unroll
   for (int i = 0; i < TERMS; ++i) planes[(i * rows + row) * per_row + chunk] = t[i];
 }
@@ -261,49 +427,6 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
     mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.m * g.out, g.out, m0 + wm0, n0 + wn0, g.m, g.out, false);
   else
     mx_store_tile<TM / WM, TN / WN, TY>(room, acc, lane, static_cast<TY*>(g.y), g.ldy, m0 + wm0, n0 + wn0, g.m, g.out, false);
-}
-
-// The gradient: a column of W at a time, element by element.
-template <typename T, int TERMS, typename TY>
-__global__ void __launch_bounds__(64) mx4_apply_grad_direct_kernel(MxApplyArgs g) {
-  const int tiles = g.tiles_m * g.tiles_n, split = (int)blockIdx.x / tiles, tile = (int)blockIdx.x % tiles;
-  const int m0 = tile % g.tiles_m * 16, c0 = tile / g.tiles_m * 16;
-  const int steps = (g.n + 31) / 32;
-  const int begin = (int)((int64_t)steps * split / g.splits), end = (int)((int64_t)steps * (split + 1) / g.splits);
-  const int lane = threadIdx.x & 63, l15 = lane & 15, l4 = lane >> 4;
-  const T* const x = static_cast<const T*>(g.x) + (int64_t)min(m0 + l15, g.m - 1) * g.ldx;
-  const int col = min(c0 + l15, g.k - 1);
-  float4_t acc = {0, 0, 0, 0};
-  for (int s = begin * 32; s < end * 32; s += 32) {
-    bf16x8_t t[TERMS];
-    const int left = g.n - s - l4 * 8;
-    mx_load_terms<T, TERMS>(x + s + l4 * 8, left, g.vec, t);
-    union {
-      bf16x8_t v;
-      __bf16 e[8];
-    } b;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      b.e[i] = (__bf16)0.0f;
-      if (i < left) {
-        const int64_t r = s + l4 * 8 + i;
-        const unsigned int byte = g.w.q[r * g.w.ldq + col / 2];
-        const bf16x2_t p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(byte >> (col & 1) * 4, mx_scale(g.w.s[r * g.w.lds + col / 32]), 0);
-        b.e[i] = p[0];
-      }
-    }
-#pragma unroll
-    for (int i = TERMS - 1; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[i], b.v, acc, 0, 0, 0);
-  }
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const int r = m0 + l4 * 4 + v;
-    if (r >= g.m || c0 + l15 >= g.k) continue;
-    if (g.splits > 1)
-      g.parts[((int64_t)split * g.m + r) * g.k + c0 + l15] = acc[v];
-    else
-      static_cast<TY*>(g.y)[r * g.ldy + c0 + l15] = (TY)acc[v];
-  }
 }
 
 }  // namespace dla

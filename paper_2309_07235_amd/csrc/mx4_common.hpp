@@ -10,6 +10,8 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x4u_t __attribute__((ext_vector_type(4), aligned(4)));  // 16 bytes from any dword
 
 constexpr int kMxStep = 128;                     // terms of the sum per scaled MFMA step; rows are padded to it
@@ -70,10 +72,53 @@ __device__ __forceinline__ bf16x8_t mx_values(unsigned int w, float scale) {
   return u.v;
 }
 
-// The conversions take a scale as the float whose exponent field it is; 255 has to be made the NaN that it stands for.
-__device__ __forceinline__ float mx_scale(unsigned int s) {
-  return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23);
+// Eight elements without their scale.
+__device__ __forceinline__ f16x8_t mx_values_f16(unsigned int w) {
+  union {
+    f16x2_t p[4];
+    f16x8_t v;
+  } u;
+  u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 0);
+  u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 1);
+  u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2);
+  u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3);
+  return u.v;
 }
+
+// a's upper 32 lanes for b's lower 32; a's odd rows of 16 lanes for b's even ones.  Both on the pairs of four registers turn register
+// and row over.
+__device__ __forceinline__ void swap_halves(unsigned int& a, unsigned int& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+__device__ __forceinline__ void swap_rows(unsigned int& a, unsigned int& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+
+// The value x, or what is there plus x, rounded once to element `at` of a matrix of type dt.
+template <typename T>
+__device__ __forceinline__ void store_value_as(void* c, int64_t at, float x, bool onto) {
+  T* const p = static_cast<T*>(c) + at;
+  *p = (T)(onto ? (float)*p + x : x);
+}
+__device__ __forceinline__ void store_value(void* c, int64_t at, float x, dla_dtype dt, bool onto) {
+  if (dt == DLA_F32)
+    store_value_as<float>(c, at, x, onto);
+  else if (dt == DLA_BF16)
+    store_value_as<__bf16>(c, at, x, onto);
+  else
+    store_value_as<_Float16>(c, at, x, onto);
+}
+
+// The scale in the low byte of s as the conversions take it: the float whose exponent field it is.  255 stands for a NaN there too,
+// and 0 for 2^-127.
+__device__ __forceinline__ float mx_scale(unsigned int s) { return __uint_as_float(s << 23 & 0x7f800000u); }
+
+// Its value: 1 with that scale.
+__device__ __forceinline__ float mx_scale_value(unsigned int s) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(0x22u, mx_scale(s), 0)[0]; }
 
 // The bf16 terms of x, which add up to it exactly: each takes the leading 8 bits of what the ones before it left (truncated, so
 // that the first cannot overflow).  What is not finite is the first term alone; a NaN stays one.

@@ -8,16 +8,15 @@ namespace {
 struct Tile {
   int m, n;
 };
-const Tile kTiles[] = {{16, 16}, {32, 32}, {128, 128}, {256, 256}};
+const Tile kTiles[] = {{16, 32}, {32, 32}, {48, 32}, {64, 32}, {128, 128}, {256, 256}};  // 32 columns: the direct kernels
 constexpr int kNumTiles = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
 constexpr int kMaxSplits = 32;
 
 int steps_of(int64_t k) { return (int)((k + kMxStep - 1) / kMxStep); }
 
-template <int MB, int NB, typename T>
+template <int MB>
 int launch_direct(const MxGemmArgs& g, hipStream_t stream) {
-  hipLaunchKernelGGL((mx4_gemm_direct_kernel<MB, NB, T>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(kMxDirectWaves * 64), 0,
-                     stream, g);
+  hipLaunchKernelGGL(mx4_gemm_direct_kernel<MB>, dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(kMxDirectWaves * 64), 0, stream, g);
   return launch_status(__func__);
 }
 
@@ -30,10 +29,18 @@ int launch_tile(const MxGemmArgs& g, hipStream_t stream) {
 
 template <typename T>
 int launch_typed(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
-  if (plan.tile_m == 16) return launch_direct<1, 1, T>(g, stream);
-  if (plan.tile_m == 32) return launch_direct<2, 2, T>(g, stream);
   if (plan.tile_m == 128) return launch_tile<128, 128, 2, 2, T>(g, stream);
   return launch_tile<256, 256, 2, 4, T>(g, stream);
+}
+
+int launch(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
+  switch (plan.tile_m) {
+    case 16: return launch_direct<1>(g, stream);
+    case 32: return launch_direct<2>(g, stream);
+    case 48: return launch_direct<3>(g, stream);
+    case 64: return launch_direct<4>(g, stream);
+  }
+  return g.dt == DLA_F32 ? launch_typed<float>(g, plan, stream) : g.dt == DLA_BF16 ? launch_typed<__bf16>(g, plan, stream) : launch_typed<_Float16>(g, plan, stream);
 }
 
 }  // namespace
@@ -47,7 +54,10 @@ int mx4_gemm_plan(int64_t m, int64_t n, int64_t k, const mx4_params* p, MxPlan* 
   MxPlan r = {0, 0, 0};
   if (p) r = MxPlan{p->tile_m, p->tile_n, p->splits};
   if (r.tile_m < 0 || r.tile_n < 0 || r.splits < 0 || r.splits > kMaxSplits || r.splits > steps_of(k)) return DLA_ERR_UNSUPPORTED_PARAMS;
-  if (r.tile_m == 0 && r.tile_n == 0) r.tile_m = r.tile_n = m <= 16 ? 16 : m < 128 ? 32 : m < 2048 ? 128 : 256;
+  if (r.tile_m == 0 && r.tile_n == 0) {
+    r.tile_m = m <= 64 ? (int)(m + 15) / 16 * 16 : m < 2048 ? 128 : 256;
+    r.tile_n = m <= 64 ? 32 : r.tile_m;
+  }
   bool found = false;
   for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n;
   if (!found) return DLA_ERR_UNSUPPORTED_PARAMS;
@@ -61,9 +71,8 @@ int mx4_gemm_plan(int64_t m, int64_t n, int64_t k, const mx4_params* p, MxPlan* 
 int mx4_gemm_launch(bool onto, const Mx4View& a, const Mx4View& b, void* c, int64_t ldc, int64_t k, dla_dtype dt, const MxPlan& plan,
                     float* parts, hipStream_t stream) {
   const MxGemmArgs g = {a, b, c, parts, ldc, steps_of(k), plan.splits, (a.rows + plan.tile_m - 1) / plan.tile_m,
-                        (b.rows + plan.tile_n - 1) / plan.tile_n, onto};
-  const int rc = dt == DLA_F32 ? launch_typed<float>(g, plan, stream)
-                 : dt == DLA_BF16 ? launch_typed<__bf16>(g, plan, stream) : launch_typed<_Float16>(g, plan, stream);
+                        (b.rows + plan.tile_n - 1) / plan.tile_n, dt, onto};
+  const int rc = launch(g, plan, stream);
   if (rc != DLA_SUCCESS || plan.splits == 1) return rc;
   return mx4_join_launch(parts, plan.splits, a.rows, b.rows, c, ldc, dt, onto, stream);
 }

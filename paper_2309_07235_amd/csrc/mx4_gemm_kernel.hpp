@@ -12,59 +12,80 @@ struct MxGemmArgs {
   float* parts;
   int64_t ldc;
   int steps, splits, tiles_m, tiles_n;
+  dla_dtype dt;
   bool onto;
 };
 
+// Few rows: what bounds the call is reading B once.  The operands go from memory to the matrix instructions; the eight waves of a
+// workgroup share the sum over k, each with a run of steps whose operands are loaded four steps ahead (two where four do not fit the
+// registers).
 constexpr int kMxDirectWaves = 8;
 
-// Few rows: the operands go from memory to the matrix instructions, and the eight waves of a workgroup share the sum.
-template <int MB, int NB, typename T>
+template <int MB>
 __global__ void __launch_bounds__(kMxDirectWaves * 64) mx4_gemm_direct_kernel(MxGemmArgs g) {
-  constexpr int TM = MB * 16, TN = NB * 16;
+  constexpr int NB = 2, TM = MB * 16, TN = NB * 16, U = MB <= 2 ? 4 : 2;
   __shared__ float part[kMxDirectWaves][TM * TN];
   const int tiles = g.tiles_m * g.tiles_n;
   const int split = (int)blockIdx.x / tiles, tile = (int)blockIdx.x % tiles;
   const int m0 = tile % g.tiles_m * TM, n0 = tile / g.tiles_m * TN;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l15 = lane & 15, l4 = lane >> 4;
   const int share = split * kMxDirectWaves + wave, shares = g.splits * kMxDirectWaves;
   const int begin = (int)((int64_t)g.steps * share / shares), end = (int)((int64_t)g.steps * (share + 1) / shares);
 
-  const uint8_t *aq[MB], *as[MB], *bq[NB], *bs[NB];
+  const uint8_t *q[MB + NB], *s[MB + NB];  // A's blocks of 16 rows, then B's
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int64_t r = min(m0 + i * 16 + l15, g.a.rows - 1);
-    aq[i] = g.a.q + r * g.a.ldq + l4 * 16;
-    as[i] = g.a.s + r * g.a.lds;
+  for (int i = 0; i < MB + NB; ++i) {
+    const Mx4View& v = i < MB ? g.a : g.b;
+    const int64_t r = min(i < MB ? m0 + i * 16 + l15 : n0 + (i - MB) * 16 + l15, v.rows - 1);
+    q[i] = v.q + r * v.ldq + l4 * 16;
+    s[i] = v.s + r * v.lds;
   }
+  struct Batch {
+    i32x4_t q[U][MB + NB];
+    unsigned int s[U][MB + NB];
+  };
+  auto load = [&](int from) {
+    Batch f;
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int64_t r = min(n0 + j * 16 + l15, g.b.rows - 1);
-    bq[j] = g.b.q + r * g.b.ldq + l4 * 16;
-    bs[j] = g.b.s + r * g.b.lds;
-  }
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < MB + NB; ++i) {
+        const int64_t at = min(from + u, end - 1);
+        f.q[u][i] = *reinterpret_cast<const i32x4_t*>(q[i] + at * 64);
+        f.s[u][i] = *reinterpret_cast<const unsigned int*>(s[i] + at * 4);
+      }
+    return f;
+  };
   float4_t acc[MB][NB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
-  for (int k = begin; k < end; ++k) {
-    i32x4_t a[MB], b[NB];
-    int sa[MB], sb[NB];
+  if (begin < end) {
+    auto use = [&](const Batch& f, int k) {
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      a[i] = *reinterpret_cast<const i32x4_t*>(aq[i] + (int64_t)k * 64);
-      sa[i] = (int)(*reinterpret_cast<const unsigned int*>(as[i] + (int64_t)k * 4) >> (8 * l4));
+      for (int u = 0; u < U; ++u) {
+        if (u > 0 && k + u >= end) break;
+        int sc[MB + NB];
+#pragma unroll
+        for (int i = 0; i < MB + NB; ++i) sc[i] = (int)(f.s[u][i] >> (8 * l4));
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[i][j] = mx_mma16(f.q[u][i], f.q[u][MB + j], acc[i][j], sc[i], sc[MB + j]);
+      }
+    };
+    // (two batches by turns: a copy from one to the other would wait for the loads)
+    Batch even = load(begin), odd;
+    for (int k = begin;; k += 2 * U) {
+      odd = load(k + U);
+      use(even, k);
+      if (k + U >= end) break;
+      even = load(k + 2 * U);
+      use(odd, k + U);
+      if (k + 2 * U >= end) break;
     }
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      b[j] = *reinterpret_cast<const i32x4_t*>(bq[j] + (int64_t)k * 64);
-      sb[j] = (int)(*reinterpret_cast<const unsigned int*>(bs[j] + (int64_t)k * 4) >> (8 * l4));
-    }
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int j = 0; j < NB; ++j) acc[i][j] = mx_mma16(a[i], b[j], acc[i][j], sa[i], sb[j]);
   }
 #pragma unroll
   for (int i = 0; i < MB; ++i)
@@ -79,12 +100,10 @@ __global__ void __launch_bounds__(kMxDirectWaves * 64) mx4_gemm_direct_kernel(Mx
     float sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < kMxDirectWaves; ++w) sum += part[w][e];
-    if (g.splits > 1) {
+    if (g.splits > 1)
       g.parts[((int64_t)split * g.a.rows + r) * g.b.rows + c] = sum;
-    } else {
-      T* const out = static_cast<T*>(g.c) + r * g.ldc + c;
-      *out = (T)(g.onto ? (float)*out + sum : sum);
-    }
+    else
+      store_value(g.c, (int64_t)r * g.ldc + c, sum, g.dt, g.onto);
   }
 }
 

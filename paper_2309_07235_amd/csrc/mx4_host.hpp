@@ -27,7 +27,7 @@ int mx4_apply_menu(int op, dla_dtype dt, mx4_params* out, int cap);
 int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const mx4_params* p, MxPlan* plan);
 int mx4_apply_launch(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, const Mx4View& w, int64_t k, void* y, int64_t ldy,
                      dla_dtype dt_y, const MxPlan& plan, void* workspace, hipStream_t stream);
-size_t mx4_apply_bytes(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const MxPlan& plan);
+size_t mx4_apply_bytes(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, int64_t n, int64_t k, const MxPlan& plan);
 
 inline size_t mx4_parts_bytes(int64_t m, int64_t n, const MxPlan& plan) {
   return plan.splits > 1 ? ((size_t)plan.splits * (size_t)m * (size_t)n * 4 + 255) / 256 * 256 : 0;

@@ -19,6 +19,14 @@ __device__ __forceinline__ unsigned int lds_offset(const void* p) {
   return __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
 }
 
+// Waits until at most N of the wave's loads are in flight; until its LDS accesses are done.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Waits until at most N of the wave's loads are in flight and all its LDS accesses are done, then for the other waves.
 template <int N>
 __device__ __forceinline__ void wait_loads_and_barrier() {
