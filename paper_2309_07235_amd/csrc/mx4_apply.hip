@@ -43,21 +43,25 @@ int launch_direct_as(const MxApplyArgs& g, hipStream_t stream) {
   return launch_status(__func__);
 }
 
-// How many waves and how far ahead is what the LDS holds.  One load of X takes four rows of 16-bit elements or two of fp32.
+// How many waves and how far ahead is what the LDS holds: of 16-bit rows up to 16, eight waves where there is one workgroup for each
+// of the 256 units at most, and four, so that two fit a unit, where there are more.  A load of X takes four rows of 16-bit
+// elements or two of fp32.
 template <typename T>
 int launch_direct(const MxApplyArgs& g, int tile_m, hipStream_t stream) {
-  constexpr bool wide_t = sizeof(T) == 4;
-  switch (tile_m) {
-    case 16:
-      if (g.m <= (wide_t ? 2 : 4)) return launch_direct_as<T, 1, 1, wide_t ? 4 : 8, 4>(g, stream);
-      return launch_direct_as<T, 1, wide_t ? 8 : 4, wide_t ? 4 : 8, 4>(g, stream);
-    case 32: return launch_direct_as<T, 2, wide_t ? 16 : 8, 4, wide_t ? 3 : 6>(g, stream);
+  if constexpr (sizeof(T) == 4) {
+    if (tile_m == 16) return g.m <= 2 ? launch_direct_as<T, 1, 1, 4, 4>(g, stream) : launch_direct_as<T, 1, 8, 4, 4>(g, stream);
+    return launch_direct_as<T, 2, 16, 4, 3>(g, stream);
+  } else {
+    const bool many = (int64_t)g.tiles_m * g.tiles_n * g.splits > 256;
+    switch (tile_m) {
+      case 16:
+        if (g.m <= 4) return many ? launch_direct_as<T, 1, 1, 4, 4>(g, stream) : launch_direct_as<T, 1, 1, 8, 4>(g, stream);
+        return many ? launch_direct_as<T, 1, 4, 4, 4>(g, stream) : launch_direct_as<T, 1, 4, 8, 4>(g, stream);
+      case 32: return launch_direct_as<T, 2, 8, 4, 6>(g, stream);
+      case 48: return launch_direct_as<T, 3, 12, 4, 6>(g, stream);
+      default: return launch_direct_as<T, 4, 16, 4, 3>(g, stream);
+    }
   }
-  if constexpr (!wide_t) {
-    if (tile_m == 48) return launch_direct_as<T, 3, 12, 4, 6>(g, stream);
-    if (tile_m == 64) return launch_direct_as<T, 4, 16, 4, 3>(g, stream);
-  }
-  return DLA_ERR_UNSUPPORTED_PARAMS;
 }
 
 template <typename T>

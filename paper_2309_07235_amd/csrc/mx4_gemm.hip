@@ -14,9 +14,15 @@ constexpr int kMaxSplits = 32;
 
 int steps_of(int64_t k) { return (int)((k + kMxStep - 1) / kMxStep); }
 
-template <int MB>
+// Eight waves a workgroup where there is one for each of the 256 units at most; four, so that two workgroups fit a unit's LDS, where
+// there are more (one row by 16384 x 4096 DIRECT_A us against DIRECT_B, by 8192 x 8192 DIRECT_C against DIRECT_D).
+template <int MB, int D8, int D4>
 int launch_direct(const MxGemmArgs& g, hipStream_t stream) {
-  hipLaunchKernelGGL(mx4_gemm_direct_kernel<MB>, dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(kMxDirectWaves * 64), 0, stream, g);
+  const unsigned grid = (unsigned)(g.tiles_m * g.tiles_n * g.splits);
+  if (grid <= 256)
+    hipLaunchKernelGGL((mx4_gemm_direct_kernel<MB, D8, 8>), dim3(grid), dim3(512), 0, stream, g);
+  else
+    hipLaunchKernelGGL((mx4_gemm_direct_kernel<MB, D4, 4>), dim3(grid), dim3(256), 0, stream, g);
   return launch_status(__func__);
 }
 
@@ -35,10 +41,10 @@ int launch_typed(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
 
 int launch(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
   switch (plan.tile_m) {
-    case 16: return launch_direct<1>(g, stream);
-    case 32: return launch_direct<2>(g, stream);
-    case 48: return launch_direct<3>(g, stream);
-    case 64: return launch_direct<4>(g, stream);
+    case 16: return launch_direct<1, 4, 4>(g, stream);
+    case 32: return launch_direct<2, 4, 4>(g, stream);
+    case 48: return launch_direct<3, 3, 3>(g, stream);
+    case 64: return launch_direct<4, 2, 2>(g, stream);
   }
   return g.dt == DLA_F32 ? launch_typed<float>(g, plan, stream) : g.dt == DLA_BF16 ? launch_typed<__bf16>(g, plan, stream) : launch_typed<_Float16>(g, plan, stream);
 }

@@ -16,46 +16,52 @@ struct MxGemmArgs {
   bool onto;
 };
 
-// Few rows: what bounds the call is reading B once.  The operands go from memory to the matrix instructions; the eight waves of a
-// workgroup share the sum over k, each with a run of steps whose operands are loaded four steps ahead (two where four do not fit the
-// registers).
-constexpr int kMxDirectWaves = 8;
-
-template <int MB>
-__global__ void __launch_bounds__(kMxDirectWaves * 64) mx4_gemm_direct_kernel(MxGemmArgs g) {
-  constexpr int NB = 2, TM = MB * 16, TN = NB * 16, U = MB <= 2 ? 4 : 2;
-  __shared__ float part[kMxDirectWaves][TM * TN];
+// Few rows: what bounds the call is reading B once.  The WV waves of a workgroup share the sum over k, each with a run of steps and LDS
+// of its own, to which both operands are loaded D steps ahead.  Through LDS, because the matrix instructions want neighbouring
+// lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16.
+template <int MB, int D, int WV>
+__global__ void __launch_bounds__(WV * 64) mx4_gemm_direct_kernel(MxGemmArgs g) {
+  constexpr int NB = 2, F = MB + NB, TM = MB * 16, TN = NB * 16;
+  constexpr int RING = D * F * 64 + 2 * F * 16;  // units of 16 bytes: the steps, and the scales of twice four
+  static_assert(WV * RING * 16 <= 160 * 1024 && RING * 16 >= TM * TN * 4, "LDS");
+  __shared__ u32x4_t lds[WV * RING];
   const int tiles = g.tiles_m * g.tiles_n;
   const int split = (int)blockIdx.x / tiles, tile = (int)blockIdx.x % tiles;
   const int m0 = tile % g.tiles_m * TM, n0 = tile / g.tiles_m * TN;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l15 = lane & 15, l4 = lane >> 4;
-  const int share = split * kMxDirectWaves + wave, shares = g.splits * kMxDirectWaves;
+  const int share = split * WV + wave, shares = g.splits * WV;
   const int begin = (int)((int64_t)g.steps * share / shares), end = (int)((int64_t)g.steps * (share + 1) / shares);
+  u32x4_t* const ring = lds + wave * RING;
+  const unsigned int at_q = lds_offset(ring), at_s = at_q + D * F * 1024;
 
-  const uint8_t *q[MB + NB], *s[MB + NB];  // A's blocks of 16 rows, then B's
+  // A's blocks of 16 rows, then B's.  A load fills one block's rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4.
+  const uint8_t* const aq = g.a.q + (int64_t)m0 * g.a.ldq;
+  const uint8_t* const bq = g.b.q + (int64_t)n0 * g.b.ldq;
+  const uint8_t* const as = g.a.s + (int64_t)m0 * g.a.lds;
+  const uint8_t* const bs = g.b.s + (int64_t)n0 * g.b.lds;
+  unsigned int qoff[F];
 #pragma unroll
-  for (int i = 0; i < MB + NB; ++i) {
-    const Mx4View& v = i < MB ? g.a : g.b;
-    const int64_t r = min(i < MB ? m0 + i * 16 + l15 : n0 + (i - MB) * 16 + l15, v.rows - 1);
-    q[i] = v.q + r * v.ldq + l4 * 16;
-    s[i] = v.s + r * v.lds;
+  for (int f = 0; f < F; ++f) {
+    const int r = lane / 4;
+    qoff[f] = (unsigned int)(f < MB ? min(f * 16 + r, g.a.rows - 1 - m0) * (int)g.a.ldq : min((f - MB) * 16 + r, g.b.rows - 1 - n0) * (int)g.b.ldq) +
+              ((lane & 3) ^ (lane >> 4)) * 16;
   }
-  struct Batch {
-    i32x4_t q[U][MB + NB];
-    unsigned int s[U][MB + NB];
+  // the scales: rows of A (MB * 16 lanes), rows of B (NB * 16)
+  const unsigned int aoff = (unsigned int)(min(lane, g.a.rows - 1 - m0) * (int)g.a.lds), boff = (unsigned int)(min(lane & 31, g.b.rows - 1 - n0) * (int)g.b.lds);
+  // (loads past the end repeat its last step, so that their number in flight is always the same)
+  auto load = [&](int s, int slot) {
+    const int64_t from = (int64_t)min(s, end - 1) * 64;
+#pragma unroll
+    for (int f = 0; f < F; ++f) load_to_lds((f < MB ? aq : bq) + from, qoff[f], at_q + (slot * F + f) * 1024);
   };
-  auto load = [&](int from) {
-    Batch f;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < MB + NB; ++i) {
-        const int64_t at = min(from + u, end - 1);
-        f.q[u][i] = *reinterpret_cast<const i32x4_t*>(q[i] + at * 64);
-        f.s[u][i] = *reinterpret_cast<const unsigned int*>(s[i] + at * 4);
-      }
-    return f;
+  // of four steps, 16 bytes a row, moved back to begin at most four steps before the row's end
+  auto scales_from = [&](int chunk) { return min(begin + chunk * 4, g.steps - 4); };
+  auto load_s = [&](int chunk) {
+    const int64_t from = (int64_t)scales_from(chunk) * 4;
+    const unsigned int to = at_s + (chunk & 1) * F * 256;
+    if (lane < TM) load_to_lds(as + from, aoff, to);
+    if (lane < TN) load_to_lds(bs + from, boff, to + MB * 256);
   };
   float4_t acc[MB][NB];
 #pragma unroll
@@ -63,43 +69,59 @@ __global__ void __launch_bounds__(kMxDirectWaves * 64) mx4_gemm_direct_kernel(Mx
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = float4_t{0, 0, 0, 0};
   if (begin < end) {
-    auto use = [&](const Batch& f, int k) {
+    if (g.steps >= 4) {
+      load_s(0);
+    } else {
+      u32x4_t a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (u > 0 && k + u >= end) break;
-        int sc[MB + NB];
+      for (int i = 0; i < 3; ++i)
+        if (begin + i < end) {
+          a[i] = *reinterpret_cast<const unsigned int*>(as + aoff + (begin + i) * 4);
+          b[i] = *reinterpret_cast<const unsigned int*>(bs + boff + (begin + i) * 4);
+        }
+      if (lane < TM) ring[D * F * 64 + lane] = a;
+      if (lane < TN) ring[D * F * 64 + TM + lane] = b;
+    }
 #pragma unroll
-        for (int i = 0; i < MB + NB; ++i) sc[i] = (int)(f.s[u][i] >> (8 * l4));
+    for (int i = 0; i < D; ++i) load(begin + i, i);
+    int slot = 0;
+    for (int s = begin; s < end; ++s) {
+      const int i = s - begin, chunk = i >> 2;
+      wait_loads<(D - 1) * F>();
+      const u32x4_t* const qr = ring + slot * F * 64;
+      const unsigned int* const sr = reinterpret_cast<const unsigned int*>(ring + D * F * 64 + (chunk & 1) * F * 16) + (g.steps >= 4 ? s - scales_from(chunk) : i);
+      i32x4_t q[F];
+      int sc[F];
 #pragma unroll
-        for (int i = 0; i < MB; ++i)
-#pragma unroll
-          for (int j = 0; j < NB; ++j) acc[i][j] = mx_mma16(f.q[u][i], f.q[u][MB + j], acc[i][j], sc[i], sc[MB + j]);
+      for (int f = 0; f < F; ++f) {
+        q[f] = __builtin_bit_cast(i32x4_t, qr[f * 64 + l15 * 4 + (l4 ^ (l15 >> 2))]);
+        sc[f] = (int)(sr[(f * 16 + l15) * 4] >> (8 * l4));
       }
-    };
-    // (two batches by turns: a copy from one to the other would wait for the loads)
-    Batch even = load(begin), odd;
-    for (int k = begin;; k += 2 * U) {
-      odd = load(k + U);
-      use(even, k);
-      if (k + U >= end) break;
-      even = load(k + 2 * U);
-      use(odd, k + U);
-      if (k + 2 * U >= end) break;
+      wait_lds();  // (before what was read is overwritten)
+      if ((i & 3) == 0 && s + 4 < end) load_s(chunk + 1);
+      load(s + D, slot);
+      slot = slot + 1 == D ? 0 : slot + 1;
+#pragma unroll
+      for (int a = 0; a < MB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[a][b] = mx_mma16(q[a], q[MB + b], acc[a][b], sc[a], sc[MB + b]);
     }
   }
+  wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
+  float* const part = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) part[wave][(i * 16 + l4 * 4 + v) * TN + j * 16 + l15] = acc[i][j][v];
+      for (int v = 0; v < 4; ++v) part[wave * TM * TN + (i * 16 + l4 * 4 + v) * TN + j * 16 + l15] = acc[i][j][v];
   __syncthreads();
-  for (int e = threadIdx.x; e < TM * TN; e += kMxDirectWaves * 64) {
+  for (int e = threadIdx.x; e < TM * TN; e += WV * 64) {
     const int r = m0 + e / TN, c = n0 + e % TN;
     if (r >= g.a.rows || c >= g.b.rows) continue;
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kMxDirectWaves; ++w) sum += part[w][e];
+    for (int w = 0; w < WV; ++w) sum += part[w * TM * TN + e];
     if (g.splits > 1)
       g.parts[((int64_t)split * g.a.rows + r) * g.b.rows + c] = sum;
     else
