@@ -11,7 +11,7 @@ constexpr int kDirect = 32;  // columns of a direct kernel's tile
 struct Tile {
   int m, n;
 };
-const Tile kTiles[] = {{16, kDirect}, {32, kDirect}, {48, kDirect}, {64, kDirect}, {128, 128}, {256, 256}};
+const Tile kTiles[] = {{16, kDirect}, {32, kDirect}, {48, kDirect}, {64, kDirect}, {32, 128}, {64, 128}, {128, 128}, {256, 256}};
 
 // The direct kernels are for op 0; more than 32 rows of fp32, or two or three terms of 256 rows, do not fit the LDS.
 bool legal(const Tile& t, int op, dla_dtype dt) {
@@ -112,6 +112,8 @@ int launch_typed(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w
   if constexpr (DT == DLA_BF16) {
     if (plan.tile_m == 256) return launch_tile<256, 256, 2, 4, 1, TY>(op, g, stream);
   }
+  if (plan.tile_m == 32) return launch_tile<32, 128, 1, 4, MxType<DT>::kTerms, TY>(op, g, stream);
+  if (plan.tile_m == 64) return launch_tile<64, 128, 1, 4, MxType<DT>::kTerms, TY>(op, g, stream);
   return launch_tile<128, 128, 2, 2, MxType<DT>::kTerms, TY>(op, g, stream);
 }
 
@@ -156,8 +158,8 @@ int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const 
   if (r.tile_m < 0 || r.tile_n < 0 || r.splits < 0 || r.splits > kMaxSplits || r.splits > (terms + kMxStep - 1) / kMxStep) return DLA_ERR_UNSUPPORTED_PARAMS;
   if (r.tile_m == 0 && r.tile_n == 0) {
     const bool direct = op == 0 && m <= (dt == DLA_F32 ? 32 : 64);
-    r.tile_m = direct ? (int)(m + 15) / 16 * 16 : m < 1024 || dt != DLA_BF16 ? 128 : 256;
-    r.tile_n = direct ? kDirect : r.tile_m;
+    r.tile_m = direct ? (int)(m + 15) / 16 * 16 : m <= 32 ? 32 : m <= 64 ? 64 : m < 1024 || dt != DLA_BF16 ? 128 : 256;
+    r.tile_n = direct ? kDirect : r.tile_m < 128 ? 128 : r.tile_m;
   }
   bool found = false;
   for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n && legal(t, op, dt);

@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
   static_assert(TN * 2 == NT, "one thread takes one block of 32 elements of W a step");
   constexpr int XS = TM * 8, WS = TN * 8;             // units of 16 bytes: a row is 64 terms
   __shared__ u32x4_t lds[2 * (TERMS * XS + WS)];
-  static_assert(2 * (TERMS * XS + WS) >= WM * WN * 1024, "16 KB a wave for the result");
+  static_assert(2 * (TERMS * XS + WS) >= WM * WN * kMxRoom<TM / WM, TN / WN>, "room for the result");
   const int tiles = g.tiles_m * g.tiles_n, split = (int)blockIdx.x / tiles;
   int ti, tj;
   tile_at(xcd_contiguous_id((int)blockIdx.x % tiles, tiles), g.tiles_m, g.tiles_n, &ti, &tj);
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
     multiply(s & 1);
   }
   wait_loads_and_barrier<0>();
-  u32x4_t* const room = lds + wave * 1024;
+  u32x4_t* const room = lds + wave * kMxRoom<TM / WM, TN / WN>;
   if (g.splits > 1)
     mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.m * g.out, g.out, m0 + wm0, n0 + wn0, g.m, g.out, false);
   else

@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
   constexpr int NT = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr int LA = TM * 4 / NT, LB = TN * 4 / NT;  // loads of 16 bytes per thread and step
   static_assert(TM + TN == NT, "one thread per row loads its scales");
-  static_assert((TM + TN) * 16 >= WM * WN * 1024, "16 KB a wave for the result");
+  static_assert((TM + TN) * 16 >= WM * WN * kMxRoom<TM / WM, TN / WN>, "room for the result");
   constexpr int STAGE = (TM + TN) * 4;               // a step's rows of both operands, in units of 16 bytes
   __shared__ u32x4_t rows[4 * STAGE];
   __shared__ u32x4_t scales[2][TM + TN];             // those of four steps at a time, 16 bytes a row
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
   }
   wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
 
-  u32x4_t* const room = rows + wave * 1024;
+  u32x4_t* const room = rows + wave * kMxRoom<TM / WM, TN / WN>;
   if (g.splits > 1)
     mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.a.rows * g.b.rows, g.b.rows, m0 + wm0, n0 + wn0, g.a.rows, g.b.rows,
                                            false);

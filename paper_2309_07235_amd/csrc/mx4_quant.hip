@@ -151,14 +151,18 @@ __global__ void __launch_bounds__(256) dequantize_kernel(Mx4View w, int64_t cols
   }
 }
 
-template <typename T>
+// C = or += the sum of the parts, PER neighbours a thread (4 where the columns are a multiple of 4).
+template <typename T, int PER>
 __global__ void __launch_bounds__(256) join_kernel(const float* parts, int splits, int64_t total, int64_t n, T* c, int64_t ldc, bool onto) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  typedef float run_t __attribute__((ext_vector_type(PER)));
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * PER;
   if (i >= total) return;
-  float sum = 0.0f;
-  for (int p = 0; p < splits; ++p) sum += parts[p * total + i];
+  run_t sum = *reinterpret_cast<const run_t*>(parts + i);
+#pragma unroll 4
+  for (int p = 1; p < splits; ++p) sum += *reinterpret_cast<const run_t*>(parts + p * total + i);
   T* const out = c + (i / n) * ldc + i % n;
-  *out = (T)(onto ? (float)*out + sum : sum);
+#pragma unroll
+  for (int v = 0; v < PER; ++v) out[v] = (T)(onto ? (float)out[v] + sum[v] : sum[v]);
 }
 
 template <typename T>
@@ -205,9 +209,13 @@ int dequantize_typed(const Mx4View& w, int64_t cols, T* y, int64_t ldy, hipStrea
 
 template <typename T>
 int join_typed(const float* parts, int splits, int64_t m, int64_t n, T* c, int64_t ldc, bool onto, hipStream_t stream) {
-  const unsigned int grid = grid_for(m * n, 256);
+  const int per = n % 4 == 0 ? 4 : 1;
+  const unsigned int grid = grid_for(m * n, 256 * per);
   if (!grid) return DLA_ERR_TOO_LARGE;
-  hipLaunchKernelGGL(join_kernel<T>, dim3(grid), dim3(256), 0, stream, parts, splits, m * n, n, c, ldc, onto);
+  if (per == 4)
+    hipLaunchKernelGGL((join_kernel<T, 4>), dim3(grid), dim3(256), 0, stream, parts, splits, m * n, n, c, ldc, onto);
+  else
+    hipLaunchKernelGGL((join_kernel<T, 1>), dim3(grid), dim3(256), 0, stream, parts, splits, m * n, n, c, ldc, onto);
   return launch_status(__func__);
 }
 

@@ -42,8 +42,11 @@ __device__ __forceinline__ void tile_at(int id, int tiles_m, int tiles_n, int* t
   *tj = in / height;
 }
 
+template <int R, int C>
+constexpr int kMxRoom = R * C / 4 < 1024 ? R * C / 4 : 1024;
+
 // A wave's part of the result, R x C in 32 x 32 blocks whose lanes hold neighbouring columns, to rows r0.. and columns c0.. of a
-// matrix of `rows` x `cols`; `lds` is the wave's own room, 1024 units of 16 bytes.  It goes through LDS as S, rounded to T (or in
+// matrix of `rows` x `cols`; `lds` is the wave's own room, kMxRoom<R, C> units of 16 bytes.  It goes through LDS as S, rounded to T (or in
 // fp32 where it is added onto C, which is rounded once), so that rows are written 16 bytes a lane.
 template <int R, int C, typename S, typename T>
 __device__ __forceinline__ void mx_store_tile(u32x4_t* lds, const f32x16_t (&acc)[R / 32][C / 32], int lane, T* c, int64_t ldc, int r0, int c0, int rows,
