@@ -87,9 +87,9 @@ template <int TM, int TN, int WM, int WN, int TERMS, typename TY>
 int launch_tile(int op, const MxApplyTileArgs& g, hipStream_t stream) {
   const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * g.splits)), block(WM * WN * 64);
   if (op == 0)
-    hipLaunchKernelGGL((mx4_apply_tile_kernel<TM, TN, WM, WN, TERMS, false, TY>), grid, block, 0, stream, g);
+    hipLaunchKernelGGL((mx4_apply_tile_kernel<TM, TN, WM, WN, TERMS, TY>), grid, block, 0, stream, g);
   else
-    hipLaunchKernelGGL((mx4_apply_tile_kernel<TM, TN, WM, WN, TERMS, true, TY>), grid, block, 0, stream, g);
+    hipLaunchKernelGGL((mx4_apply_grad_kernel<TM, TN, WM, WN, TERMS, TY>), grid, block, 0, stream, g);
   return launch_status(__func__);
 }
 

@@ -286,13 +286,168 @@ struct MxApplyTileArgs {
   int steps, splits, tiles_m, tiles_n;  // steps of 64 terms
 };
 
-// A tile of Y.  X's rows go to LDS as they are; W's elements become bf16 on their way there, once per workgroup, with the terms of
-// the sum neighbours in a row in both operations: GRAD turns blocks of 4 rows by 8 columns over in registers.
-template <int TM, int TN, int WM, int WN, int TERMS, bool GRAD, typename TY>
+// How many steps of a tile of Y = X*W^T the LDS holds: up to six where two workgroups of a unit can have them, else as many as one can.
+constexpr int apply_depth(int tm, int tn, int terms) {
+  const int stage = tm * 128 * terms + tn * 32, scales = tn * 32;
+  const int shared = (80 * 1024 - scales) / stage, alone = (160 * 1024 - scales) / stage;
+  return shared >= 3 ? (shared > 6 ? 6 : shared) : (alone > 4 ? 4 : alone);
+}
+
+// A tile of Y = X*W^T.  X's rows and W's go to LDS as they are, a ring of D steps of 64 terms; a wave makes its part of W bf16 as it
+// takes it to its registers (every element in WM waves).  A lane holds one block of a row of W, instruction j takes its elements
+// 8 j .. 8 j + 7, and X's likewise.
+template <int TM, int TN, int WM, int WN, int TERMS, typename TY>
 __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTileArgs g) {
+  constexpr int NW = WM * WN, FM = TM / WM / 32, FN = TN / WN / 32, D = apply_depth(TM, TN, TERMS);
+  constexpr int LX = TM / 8 / NW, LW = TN / 32 / NW;             // loads of X (a plane) and of W per wave and step
+  static_assert(LX * NW * 8 == TM && LW * NW * 32 == TN && TN <= NW * 64 && D >= 2, "whole loads");
+  constexpr int XS = TM * 8, WS = TN * 2, STAGE = TERMS * XS + WS;  // units of 16 bytes
+  __shared__ u32x4_t lds[D * STAGE + 2 * TN];                     // the steps; the scales of twice eight steps, 16 bytes a row
+  static_assert(D * STAGE + 2 * TN >= NW * kMxRoom<TM / WM, TN / WN>, "room for the result");
+  const int tiles = g.tiles_m * g.tiles_n, split = (int)blockIdx.x / tiles;
+  int ti, tj;
+  tile_at(xcd_contiguous_id((int)blockIdx.x % tiles, tiles), g.tiles_m, g.tiles_n, &ti, &tj);
+  const int m0 = ti * TM, n0 = tj * TN;
+  const int pairs = (g.steps + 1) / 2;  // a share begins at a whole 128 terms
+  const int first = 2 * (int)((int64_t)pairs * split / g.splits), steps = min(g.steps, 2 * (int)((int64_t)pairs * (split + 1) / g.splits)) - first;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l31 = lane & 31, l5 = lane >> 5;
+  const int wm0 = wave / WN * (TM / WM), wn0 = wave % WN * (TN / WN);
+
+  // X: a load fills eight rows, chunk c of row r at c ^ r / 2 % 8 (the 16 rows that are read at one chunk take all banks).  W: 32 rows.
+  const __bf16* const xb = g.x + (int64_t)m0 * g.ldx + (int64_t)first * 64;
+  const uint8_t* const wb = g.w.q + (int64_t)n0 * g.w.ldq + (int64_t)first * 32;
+  unsigned int xoff[LX], woff[LW];
+#pragma unroll
+  for (int i = 0; i < LX; ++i) {
+    const int r = (wave * LX + i) * 8 + lane / 8;
+    xoff[i] = (unsigned int)min(r, g.m - 1 - m0) * (unsigned int)(g.ldx * 2) + ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < LW; ++i) woff[i] = (unsigned int)(min((wave * LW + i) * 32 + lane / 2, g.w.rows - 1 - n0) * (int)g.w.ldq) + (lane & 1) * 16;
+  const unsigned int lds0 = lds_offset(lds);
+  // (loads past the last step repeat it, so that their number in flight is always the same)
+  auto load = [&](int s, int slot) {
+    const int64_t at = min(s, steps - 1);
+    const unsigned int to = lds0 + slot * STAGE * 16;
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < LX; ++i) load_to_lds(xb + t * g.plane + at * 64, xoff[i], to + (t * XS + (wave * LX + i) * 64) * 16);
+#pragma unroll
+    for (int i = 0; i < LW; ++i) load_to_lds(wb + at * 32, woff[i], to + (TERMS * XS + (wave * LW + i) * 64) * 16);
+  };
+  // the scales of eight steps, a thread a row, moved back to begin at most sixteen bytes before the row's end
+  const bool scaler = wave * 64 < TN;
+  const uint8_t* const sp = g.w.s + (int64_t)n0 * g.w.lds;
+  const unsigned int soff = (unsigned int)(min(tid, g.w.rows - 1 - n0) * (int)g.w.lds);
+  const int blocks = pairs * 4;         // of 32 terms in a row with its padding
+  auto scales_from = [&](int chunk) { return min(first * 2 + chunk * 16, blocks - 16); };
+  auto load_scales = [&](int chunk) {
+    if (scaler) load_to_lds(sp + scales_from(chunk), soff, lds0 + (D * STAGE + (chunk & 1) * TN + wave * 64) * 16);
+  };
+
+  f32x16_t acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+  struct Part {
+    bf16x8_t x[TERMS][FM];
+  };
+  struct Weights {
+    u32x4_t q[FN];
+    float s[FN];
+  };
+  auto read_x = [&](int slot, int j) {
+    Part f;
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int r = wm0 + i * 32 + l31;
+        f.x[t][i] = __builtin_bit_cast(bf16x8_t, lds[slot * STAGE + t * XS + r * 8 + ((l5 * 4 + j) ^ ((r >> 1) & 7))]);
+      }
+    return f;
+  };
+  auto read_w = [&](int s, int slot) {
+    Weights f;
+    const uint8_t* const sc = reinterpret_cast<const uint8_t*>(lds + D * STAGE + ((s >> 3) & 1) * TN) + (blocks >= 16 ? (first + s) * 2 - scales_from(s >> 3) : s * 2) + l5;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int r = wn0 + j * 32 + l31;
+      f.q[j] = lds[slot * STAGE + TERMS * XS + r * 2 + l5];
+      f.s[j] = mx_scale(sc[r * 16]);
+    }
+    return f;
+  };
+  auto multiply = [&](const Part& f, const Weights& w, int j) {
+    bf16x8_t b[FN];
+#pragma unroll
+    for (int n = 0; n < FN; ++n) b[n] = mx_values(w.q[n][j], w.s[n]);
+#pragma unroll
+    for (int t = TERMS - 1; t >= 0; --t)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int n = 0; n < FN; ++n) acc[i][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[n], f.x[t][i], acc[i][n], 0, 0, 0);
+    // (an empty use of the sums: what follows is not moved in front of the products)
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int n = 0; n < FN; ++n) asm volatile("" : "+v"(acc[i][n]));
+  };
+
+  if (blocks >= 16) {
+    load_scales(0);
+  } else if (tid < TN) {
+    u32x4_t w = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i * 2 < steps) w[i] = *reinterpret_cast<const unsigned int*>(sp + soff + first * 2 + i * 4);
+    lds[D * STAGE + tid] = w;
+  }
+  // D steps are on their way; the waves meet in the last quarter of a step, when the next one has arrived and nobody reads this one any more
+  constexpr int L = TERMS * LX + LW;
+#pragma unroll
+  for (int i = 0; i < D; ++i) load(i, i);
+  wait_loads_and_barrier<(D - 1) * L>();
+  Weights w = read_w(0, 0);
+  Part even = read_x(0, 0), odd;
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    odd = read_x(slot, 1);
+    multiply(even, w, 0);
+    even = read_x(slot, 2);
+    multiply(odd, w, 1);
+    odd = read_x(slot, 3);
+    multiply(even, w, 2);
+    wait_loads_and_barrier<(D - 2) * L>();
+    if ((s & 7) == 0 && s + 8 < steps) load_scales(s / 8 + 1);  // its buffer was last read before step s - 1's barrier
+    load(s + D, slot);
+    slot = slot + 1 == D ? 0 : slot + 1;
+    const Weights next = read_w(min(s + 1, steps - 1), slot);
+    even = read_x(slot, 0);
+    multiply(odd, w, 3);
+    w = next;
+  }
+  wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
+  u32x4_t* const room = lds + wave * kMxRoom<TM / WM, TN / WN>;
+  if (g.splits > 1)
+    mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.m * g.out, g.out, m0 + wm0, n0 + wn0, g.m, g.out, false);
+  else
+    mx_store_tile<TM / WM, TN / WN, TY>(room, acc, lane, static_cast<TY*>(g.y), g.ldy, m0 + wm0, n0 + wn0, g.m, g.out, false);
+}
+
+// A tile of Y = X*W.  X's rows go to LDS as they are; W's elements become bf16 on their way there, once per workgroup, turned over in
+// registers in blocks of 4 rows by 8 columns, so that the terms of the sum are neighbours.
+template <int TM, int TN, int WM, int WN, int TERMS, typename TY>
+__global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTileArgs g) {
   constexpr int NT = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr int LX = TM * 8 / NT;                     // loads of 16 bytes per thread, step and plane
-  static_assert(TN * 2 == NT, "one thread takes one block of 32 elements of W a step");
+  static_assert(TN * 2 == NT, "a thread takes 32 elements of W a step");
   constexpr int XS = TM * 8, WS = TN * 8;             // units of 16 bytes: a row is 64 terms
   __shared__ u32x4_t lds[2 * (TERMS * XS + WS)];
   static_assert(2 * (TERMS * XS + WS) >= WM * WN * kMxRoom<TM / WM, TN / WN>, "room for the result");
@@ -305,7 +460,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
   const int wm0 = wave / WN * (TM / WM), wn0 = wave % WN * (TN / WN);
 
   // Chunk c of 16 bytes of row r lies at c ^ turn(r): 16 rows that are read at the same chunk take all banks, and so do the
-  // columns 8 l + i that GRAD's lanes write.
+  // columns 8 l + i that the lanes write.
   auto turn = [](int r) { return ((r >> 1) ^ (r >> 3)) & 7; };
 
   // X: a load instruction fills eight rows
@@ -325,51 +480,37 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
         load_to_lds(xb + t * g.plane + (int64_t)s * 64, xoff[i], lds0 + ((stage * TERMS + t) * XS + (wave * LX + i) * 64) * 16);
   };
 
-  // W, not GRAD: thread 2 r + h takes block h of row r.  GRAD: a thread takes columns 8 wc .. 8 wc + 7 of four rows.
+  // W: a thread takes columns 8 wc .. 8 wc + 7 of four rows
   constexpr int LPR = TN / 8;
   const int wc = tid % LPR, wr = tid / LPR * 4;
-  const int64_t wrow = min(n0 + tid / 2, g.w.rows - 1);
   const int wcol = min(n0 + wc * 8, g.w_cols - 8);
   struct Raw {
-    u32x4_t q;
-    unsigned int s[GRAD ? 4 : 1];
+    unsigned int q[4], s[4];
   };
   auto load_w = [&](int s) {
     Raw f;
-    if constexpr (GRAD) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = (first + s) * 64 + wr + i;
-        const bool there = r < g.w.rows;
-        const int64_t at = there ? r : g.w.rows - 1;
-        f.q[i] = *reinterpret_cast<const unsigned int*>(g.w.q + at * g.w.ldq + wcol / 2);
-        f.s[i] = g.w.s[at * g.w.lds + wcol / 32];
-        if (!there) f.q[i] = f.s[i] = 0;
-      }
-    } else {
-      f.q = *reinterpret_cast<const u32x4_t*>(g.w.q + wrow * g.w.ldq + (int64_t)(first + s) * 32 + (tid & 1) * 16);
-      f.s[0] = g.w.s[wrow * g.w.lds + (int64_t)(first + s) * 2 + (tid & 1)];
+    for (int i = 0; i < 4; ++i) {
+      const int r = (first + s) * 64 + wr + i;
+      const bool there = r < g.w.rows;
+      const int64_t at = there ? r : g.w.rows - 1;
+      f.q[i] = *reinterpret_cast<const unsigned int*>(g.w.q + at * g.w.ldq + wcol / 2);
+      f.s[i] = g.w.s[at * g.w.lds + wcol / 32];
+      if (!there) f.q[i] = f.s[i] = 0;
     }
     return f;
   };
   auto store_w = [&](const Raw& f, int stage) {
     u32x4_t* const to = lds + 2 * TERMS * XS + stage * WS;
-    if constexpr (GRAD) {
-      u32x4_t v[4];
+    u32x4_t v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(u32x4_t, mx_values(f.q[i], mx_scale(f.s[i])));
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(u32x4_t, mx_values(f.q[i], mx_scale(f.s[i])));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = wc * 8 + i;
-        const unsigned int sel = i & 1 ? 0x07060302u : 0x05040100u;
-        const u32x2_t w = {__builtin_amdgcn_perm(v[1][i / 2], v[0][i / 2], sel), __builtin_amdgcn_perm(v[3][i / 2], v[2][i / 2], sel)};
-        reinterpret_cast<u32x2_t*>(to + c * 8 + ((wr / 8) ^ turn(c)))[wr / 4 & 1] = w;
-      }
-    } else {
-      const float sc = mx_scale(f.s[0]);
-      const int r = tid / 2;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) to[r * 8 + (((tid & 1) * 4 + j) ^ turn(r))] = __builtin_bit_cast(u32x4_t, mx_values(f.q[j], sc));
+    for (int i = 0; i < 8; ++i) {
+      const int c = wc * 8 + i;
+      const unsigned int sel = i & 1 ? 0x07060302u : 0x05040100u;
+      const u32x2_t w = {__builtin_amdgcn_perm(v[1][i / 2], v[0][i / 2], sel), __builtin_amdgcn_perm(v[3][i / 2], v[2][i / 2], sel)};
+      reinterpret_cast<u32x2_t*>(to + c * 8 + ((wr / 8) ^ turn(c)))[wr / 4 & 1] = w;
     }
   };
 
@@ -412,9 +553,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
   for (int s = 0; s < steps; ++s) {
     wait_loads_and_barrier<0>();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(raw.q[i]));  // (the compiler's own wait for these, before more is loaded)
-#pragma unroll
-    for (int i = 0; i < (GRAD ? 4 : 1); ++i) asm volatile("" : "+v"(raw.s[i]));
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(raw.q[i]), "+v"(raw.s[i]));  // (the compiler's own wait for these, before more is loaded)
     const Raw now = raw;
     load_x(min(s + 1, steps - 1), (s + 1) & 1);
     raw = load_w(min(s + 2, steps - 1));
