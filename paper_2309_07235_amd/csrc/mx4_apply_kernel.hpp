@@ -441,16 +441,25 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
     mx_store_tile<TM / WM, TN / WN, TY>(room, acc, lane, static_cast<TY*>(g.y), g.ldy, m0 + wm0, n0 + wn0, g.m, g.out, false);
 }
 
-// A tile of Y = X*W.  X's rows go to LDS as they are; W's elements become bf16 on their way there, once per workgroup, turned over in
-// registers in blocks of 4 rows by 8 columns, so that the terms of the sum are neighbours.
+// How many steps of a tile of Y = X*W are in LDS or on their way there.
+constexpr int grad_depth(int tm, int tn, int terms) {
+  const int stage = tm * 128 * terms + tn * 32 + tn * 2, fixed = 2 * tn * 128;
+  const int shared = (80 * 1024 - fixed) / stage, alone = (160 * 1024 - fixed) / stage;
+  return shared >= 2 ? (shared > 4 ? 4 : shared) : (alone > 3 ? 3 : alone);
+}
+
+// A tile of Y = X*W.  X's rows and W's go to LDS as they are, a ring of D steps of 64 terms (rows of W).  The terms of the sum are the rows of W,
+// so what a lane needs of it is a column: a step ahead, threads turn blocks of 4 rows by 8 columns over in registers, make them bf16
+// and leave them in LDS with the terms as neighbours, once per workgroup.
 template <int TM, int TN, int WM, int WN, int TERMS, typename TY>
 __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTileArgs g) {
-  constexpr int NT = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
-  constexpr int LX = TM * 8 / NT;                     // loads of 16 bytes per thread, step and plane
-  static_assert(TN * 2 == NT, "a thread takes 32 elements of W a step");
-  constexpr int XS = TM * 8, WS = TN * 8;             // units of 16 bytes: a row is 64 terms
-  __shared__ u32x4_t lds[2 * (TERMS * XS + WS)];
-  static_assert(2 * (TERMS * XS + WS) >= WM * WN * kMxRoom<TM / WM, TN / WN>, "room for the result");
+  constexpr int NW = WM * WN, NT = NW * 64, FM = TM / WM / 32, FN = TN / WN / 32, D = grad_depth(TM, TN, TERMS);
+  constexpr int LX = TM / 8 / NW;                     // loads of X per plane, wave and step; of W's elements and scales one each
+  static_assert(LX * NW * 8 == TM && TN * 2 == NT && D >= 2, "a thread takes 32 elements of W a step");
+  constexpr int XS = TM * 8, RS = TN * 2, SS = TN / 8;   // units of 16 bytes: X's rows, W's, and the scales
+  constexpr int STAGE = TERMS * XS + RS + SS, WS = TN * 8;
+  __shared__ u32x4_t lds[D * STAGE + 2 * WS];
+  static_assert(D * STAGE + 2 * WS >= NW * kMxRoom<TM / WM, TN / WN>, "room for the result");
   const int tiles = g.tiles_m * g.tiles_n, split = (int)blockIdx.x / tiles;
   int ti, tj;
   tile_at(xcd_contiguous_id((int)blockIdx.x % tiles, tiles), g.tiles_m, g.tiles_n, &ti, &tj);
@@ -463,7 +472,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
   // columns 8 l + i that the lanes write.
   auto turn = [](int r) { return ((r >> 1) ^ (r >> 3)) & 7; };
 
-  // X: a load instruction fills eight rows
+  // X: a load fills eight rows
   const __bf16* const xb = g.x + (int64_t)m0 * g.ldx + (int64_t)first * 64;
   unsigned int xoff[LX];
 #pragma unroll
@@ -471,40 +480,45 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
     const int r = (wave * LX + i) * 8 + lane / 8;
     xoff[i] = (unsigned int)min(r, g.m - 1 - m0) * (unsigned int)(g.ldx * 2) + ((lane & 7) ^ turn(r)) * 16;
   }
+  // W: a wave's load fills 64 / RCH rows of RCH chunks.  Row 4 a + b of each 16 lies at 4 b + a, so that the threads of four rows each, which
+  // read row 4 a + b together, do so from neighbouring rows.  Columns past the padding repeat the last.
+  constexpr int RCH = TN / 32, RPL = 64 / RCH;
+  const int wslot = wave * RPL + lane / RCH, wrow = (wslot & ~15) | (wslot & 3) * 4 | (wslot >> 2 & 3);
+  const int wcol = min(n0 / 2 + lane % RCH * 16, g.w_cols / 2 - 16);
+  // and its scales: TN / 32 bytes of each of 64 rows, 16 lanes of every wave
+  constexpr int SPR = TN / 128;                       // dwords of a row
+  const int srow = (wave * 16 + (lane & 15)) / SPR, scol = min(n0 / 32 + (lane & 15) % SPR * 4, g.w_cols / 32 - 4);
   const unsigned int lds0 = lds_offset(lds);
-  auto load_x = [&](int s, int stage) {
+  // (loads past the last step or row repeat it: the number in flight is always the same; what lies behind W's rows is made zero below)
+  auto load_x = [&](int s, int slot) {
+    const int64_t at = (int64_t)min(s, steps - 1) * 64;
 #pragma unroll
     for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-      for (int i = 0; i < LX; ++i)
-        load_to_lds(xb + t * g.plane + (int64_t)s * 64, xoff[i], lds0 + ((stage * TERMS + t) * XS + (wave * LX + i) * 64) * 16);
+      for (int i = 0; i < LX; ++i) load_to_lds(xb + t * g.plane + at, xoff[i], lds0 + (slot * STAGE + t * XS + (wave * LX + i) * 64) * 16);
   };
-
-  // W: a thread takes columns 8 wc .. 8 wc + 7 of four rows
+  auto load_w = [&](int s, int slot) {
+    const int r0 = (first + min(s, steps - 1)) * 64, last = g.w.rows - 1 - r0;
+    const unsigned int to = lds0 + (slot * STAGE + TERMS * XS) * 16;
+    load_to_lds(g.w.q + (int64_t)r0 * g.w.ldq, (unsigned int)(min(wrow, last) * (int)g.w.ldq + wcol), to + wave * 1024);
+    if (lane < 16) load4_to_lds(g.w.s + (int64_t)r0 * g.w.lds, (unsigned int)(min(srow, last) * (int)g.w.lds + scol), to + RS * 16 + wave * 64);
+  };
+  // W of a step, made bf16 and turned over: columns 8 wc .. 8 wc + 7 of rows wr .. wr + 3
   constexpr int LPR = TN / 8;
   const int wc = tid % LPR, wr = tid / LPR * 4;
-  const int wcol = min(n0 + wc * 8, g.w_cols - 8);
-  struct Raw {
-    unsigned int q[4], s[4];
-  };
-  auto load_w = [&](int s) {
-    Raw f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = (first + s) * 64 + wr + i;
-      const bool there = r < g.w.rows;
-      const int64_t at = there ? r : g.w.rows - 1;
-      f.q[i] = *reinterpret_cast<const unsigned int*>(g.w.q + at * g.w.ldq + wcol / 2);
-      f.s[i] = g.w.s[at * g.w.lds + wcol / 32];
-      if (!there) f.q[i] = f.s[i] = 0;
-    }
-    return f;
-  };
-  auto store_w = [&](const Raw& f, int stage) {
-    u32x4_t* const to = lds + 2 * TERMS * XS + stage * WS;
+  auto turn_over = [&](int s, int slot) {
+    const unsigned int* const q = reinterpret_cast<const unsigned int*>(lds + slot * STAGE + TERMS * XS);
+    const uint8_t* const sc = reinterpret_cast<const uint8_t*>(lds + slot * STAGE + TERMS * XS + RS);
+    const int left = g.w.rows - (first + s) * 64;
     u32x4_t v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(u32x4_t, mx_values(f.q[i], mx_scale(f.s[i])));
+    for (int i = 0; i < 4; ++i) {
+      const int r = wr + i, at = (r & ~15) | (r & 3) * 4 | (r >> 2 & 3);
+      const bool there = r < left;
+      const unsigned int e = there ? q[at * (TN / 8) + wc] : 0u, f = there ? sc[r * (TN / 32) + wc / 4] : 0u;
+      v[i] = __builtin_bit_cast(u32x4_t, mx_values(e, mx_scale(f)));
+    }
+    u32x4_t* const to = lds + D * STAGE + (s & 1) * WS;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int c = wc * 8 + i;
@@ -522,45 +536,73 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
 
-  auto multiply = [&](int stage) {
-    const u32x4_t* const xs = lds + stage * TERMS * XS;
-    const u32x4_t* const ws = lds + 2 * TERMS * XS + stage * WS;
+  struct Part {
+    bf16x8_t x[TERMS][FM], w[FN];
+  };
+  auto read = [&](int s, int slot, int k) {
+    Part f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      bf16x8_t b[FN];
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int r = wn0 + j * 32 + l31;
-        b[j] = __builtin_bit_cast(bf16x8_t, ws[r * 8 + ((k * 2 + l5) ^ turn(r))]);
-      }
-#pragma unroll
-      for (int t = TERMS - 1; t >= 0; --t)
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const int r = wm0 + i * 32 + l31;
-          const bf16x8_t a = __builtin_bit_cast(bf16x8_t, xs[t * XS + r * 8 + ((k * 2 + l5) ^ turn(r))]);
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], a, acc[i][j], 0, 0, 0);
-        }
+    for (int j = 0; j < FN; ++j) {
+      const int r = wn0 + j * 32 + l31;
+      f.w[j] = __builtin_bit_cast(bf16x8_t, lds[D * STAGE + (s & 1) * WS + r * 8 + ((k * 2 + l5) ^ turn(r))]);
     }
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int r = wm0 + i * 32 + l31;
+        f.x[t][i] = __builtin_bit_cast(bf16x8_t, lds[slot * STAGE + t * XS + r * 8 + ((k * 2 + l5) ^ turn(r))]);
+      }
+    return f;
+  };
+  auto multiply = [&](const Part& f) {
+#pragma unroll
+    for (int t = TERMS - 1; t >= 0; --t)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[j], f.x[t][i], acc[i][j], 0, 0, 0);
+    // (an empty use of the sums: what follows is not moved in front of the products)
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
 
-  // X of the next step is on its way and W's becomes bf16 while this step is multiplied; W's of the one after is in registers
-  load_x(0, 0);
-  Raw raw = load_w(0);
-  store_w(raw, 0);
-  raw = load_w(min(1, steps - 1));
-  for (int s = 0; s < steps; ++s) {
-    wait_loads_and_barrier<0>();
+  // Loads go in groups of X of one step and W of the next; D groups are on their way.  The waves meet in the last quarter of a step:
+  // the next step's X and W, and the one's after in LDS, are there, and nobody reads this one's any more.
+  constexpr int L = TERMS * LX + 2;
+  load_w(0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(raw.q[i]), "+v"(raw.s[i]));  // (the compiler's own wait for these, before more is loaded)
-    const Raw now = raw;
-    load_x(min(s + 1, steps - 1), (s + 1) & 1);
-    raw = load_w(min(s + 2, steps - 1));
-    store_w(now, (s + 1) & 1);
-    multiply(s & 1);
+  for (int i = 0; i < D - 1; ++i) {
+    load_x(i, i);
+    load_w(i + 1, i + 1);
   }
-  wait_loads_and_barrier<0>();
+  wait_loads_and_barrier<(D - 1) * L>();
+  turn_over(0, 0);
+  wait_loads_and_barrier<(D - 1) * L>();
+  load_x(D - 1, D - 1);
+  load_w(D, 0);
+  wait_loads_and_barrier<(D - 1) * L>();
+  Part even = read(0, 0, 0), odd;
+  int slot = 0;
+  for (int s = 0; s < steps; ++s) {
+    const int after = slot + 1 == D ? 0 : slot + 1;
+    odd = read(s, slot, 1);
+    multiply(even);
+    even = read(s, slot, 2);
+    turn_over(s + 1, after);
+    multiply(odd);
+    odd = read(s, slot, 3);
+    multiply(even);
+    wait_loads_and_barrier<(D - 2) * L>();
+    load_x(s + D, slot);
+    load_w(s + 1 + D, after);
+    slot = after;
+    even = read(s + 1, slot, 0);
+    multiply(odd);
+  }
+  wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
   u32x4_t* const room = lds + wave * kMxRoom<TM / WM, TN / WN>;
   if (g.splits > 1)
     mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.m * g.out, g.out, m0 + wm0, n0 + wn0, g.m, g.out, false);

@@ -14,6 +14,12 @@ __device__ __forceinline__ void load_to_lds(const void* base, unsigned int off, 
                : "memory");
 }
 
+// The same with 4 bytes of every lane, lane l's to byte lds + 4 l.
+__device__ __forceinline__ void load4_to_lds(const void* base, unsigned int off, unsigned int lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
+               : "memory");
+}
+
 // Where an array in LDS starts, for load_to_lds.
 __device__ __forceinline__ unsigned int lds_offset(const void* p) {
   return __builtin_amdgcn_readfirstlane((unsigned int)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
