@@ -506,24 +506,30 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
   // W of a step, made bf16 and turned over: columns 8 wc .. 8 wc + 7 of rows wr .. wr + 3
   constexpr int LPR = TN / 8;
   const int wc = tid % LPR, wr = tid / LPR * 4;
-  auto turn_over = [&](int s, int slot) {
+  struct Block {
+    u32x4_t v[4];
+  };
+  auto take = [&](int s, int slot) {
     const unsigned int* const q = reinterpret_cast<const unsigned int*>(lds + slot * STAGE + TERMS * XS);
     const uint8_t* const sc = reinterpret_cast<const uint8_t*>(lds + slot * STAGE + TERMS * XS + RS);
     const int left = g.w.rows - (first + s) * 64;
-    u32x4_t v[4];
+    Block f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = wr + i, at = (r & ~15) | (r & 3) * 4 | (r >> 2 & 3);
-      const bool there = r < left;
-      const unsigned int e = there ? q[at * (TN / 8) + wc] : 0u, f = there ? sc[r * (TN / 32) + wc / 4] : 0u;
-      v[i] = __builtin_bit_cast(u32x4_t, mx_values(e, mx_scale(f)));
+      const unsigned int e = q[at * (TN / 8) + wc], x = sc[r * (TN / 32) + wc / 4];
+      const u32x4_t v = __builtin_bit_cast(u32x4_t, mx_values(e, mx_scale(x)));
+      f.v[i] = r < left ? v : u32x4_t{0, 0, 0, 0};
     }
+    return f;
+  };
+  auto turn_over = [&](const Block& f, int s, int from, int to_column) {
     u32x4_t* const to = lds + D * STAGE + (s & 1) * WS;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = from; i < to_column; ++i) {
       const int c = wc * 8 + i;
       const unsigned int sel = i & 1 ? 0x07060302u : 0x05040100u;
-      const u32x2_t w = {__builtin_amdgcn_perm(v[1][i / 2], v[0][i / 2], sel), __builtin_amdgcn_perm(v[3][i / 2], v[2][i / 2], sel)};
+      const u32x2_t w = {__builtin_amdgcn_perm(f.v[1][i / 2], f.v[0][i / 2], sel), __builtin_amdgcn_perm(f.v[3][i / 2], f.v[2][i / 2], sel)};
       reinterpret_cast<u32x2_t*>(to + c * 8 + ((wr / 8) ^ turn(c)))[wr / 4 & 1] = w;
     }
   };
@@ -562,6 +568,13 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[j], f.x[t][i], acc[i][j], 0, 0, 0);
+    // what a thread does for the next step between the products
+#pragma unroll
+    for (int i = 0; i < TERMS * FM * FN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x300, 2, 0);
+    }
     // (an empty use of the sums: what follows is not moved in front of the products)
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -579,7 +592,7 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
     load_w(i + 1, i + 1);
   }
   wait_loads_and_barrier<(D - 1) * L>();
-  turn_over(0, 0);
+  turn_over(take(0, 0), 0, 0, 8);
   wait_loads_and_barrier<(D - 1) * L>();
   load_x(D - 1, D - 1);
   load_w(D, 0);
@@ -589,11 +602,13 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
   for (int s = 0; s < steps; ++s) {
     const int after = slot + 1 == D ? 0 : slot + 1;
     odd = read(s, slot, 1);
+    const Block next = take(s + 1, after);
     multiply(even);
     even = read(s, slot, 2);
-    turn_over(s + 1, after);
+    turn_over(next, s + 1, 0, 4);
     multiply(odd);
     odd = read(s, slot, 3);
+    turn_over(next, s + 1, 4, 8);
     multiply(even);
     wait_loads_and_barrier<(D - 2) * L>();
     load_x(s + D, slot);
