@@ -1,21 +1,69 @@
 // Host side of microscaled weights applied to ordinary rows: the tile menu, the choice of a schedule and the launches.
 #include "mx4_apply_kernel.hpp"
-#include "mx4_host.hpp"
+#include "mx4_schedule.hpp"
 
 namespace dla {
 namespace {
 
-constexpr int kMaxSplits = 32;
 constexpr int kDirect = 32;  // columns of a direct kernel's tile
 
-struct Tile {
-  int m, n;
+// The tiles.  The direct kernels are for op 0; more than 32 rows of fp32 there, and two or three terms of 256 rows, do not fit the LDS.  The
+// costs are fitted to 3600 timings of 176 products (1 to 4096 rows, 128 to 8192 columns and terms, every tile, 1 to 32 splits): the choice takes
+// 1 to 6 % longer in the mean than the best of them, by operation and type.
+const MxTileCost kForwardBf16[] = {
+    {16, 32, 7.02f, 2.86f, 0.0348f, 0.0982f, 0.702f},
+    {32, 32, 7.92f, 1.94f, 0.0926f, 0.175f, 0.954f},
+    {48, 32, 7.65f, 2.03f, 0.141f, 0.256f, 0.994f},
+    {64, 32, 8.19f, 1.08f, 0.266f, 0.279f, 1.0f},
+    {32, 128, 7.67f, 0.495f, 0.502f, 0.358f, 1.42f},
+    {64, 128, 6.43f, 1.55f, 0.661f, 0.455f, 2.78f},
+    {128, 128, 6.81f, 1.36f, 1.02f, 0.782f, 2.59f},
+    {256, 256, 9.62f, 2.93f, 0.574f, 2.53f, 0.998f},
 };
-const Tile kTiles[] = {{16, kDirect}, {32, kDirect}, {48, kDirect}, {64, kDirect}, {32, 128}, {64, 128}, {128, 128}, {256, 256}};
+const MxTileCost kForwardF16[] = {
+    {16, 32, 6.86f, 3.31f, 0.0586f, 0.0792f, 0.924f},
+    {32, 32, 9.58f, 0.984f, 0.106f, 0.106f, 0.984f},
+    {48, 32, 9.34f, 1.01f, 0.162f, 0.162f, 1.01f},
+    {64, 32, 6.08f, 3.98f, 0.17f, 0.207f, 3.07f},
+    {32, 128, 9.12f, 1.48f, 0.352f, 0.576f, 1.01f},
+    {64, 128, 9.27f, 1.9f, 0.345f, 0.815f, 0.967f},
+    {128, 128, 2.83f, 8.18f, 1.61f, 0.5f, 0.994f},
+};
+const MxTileCost kForwardF32[] = {
+    {16, 32, 2.32f, 7.07f, 0.0737f, 0.314f, 2.5f},
+    {32, 32, 3.73f, 5.31f, 0.22f, 0.551f, 2.97f},
+    {32, 128, 7.17f, 3.88f, 0.306f, 0.865f, 1.0f},
+    {64, 128, 3.56f, 6.08f, 1.14f, 1.44f, 4.25f},
+    {128, 128, 7.93f, 2.94f, 0.508f, 2.63f, 1.0f},
+};
+const MxTileCost kGradBf16[] = {
+    {32, 128, 5.51f, 2.2f, 0.862f, 0.748f, 1.01f},
+    {64, 128, 6.77f, 1.03f, 1.04f, 0.869f, 0.746f},
+    {128, 128, 5.78f, 2.28f, 1.13f, 1.04f, 1.01f},
+    {256, 256, 8.44f, 2.95f, 0.507f, 2.73f, 0.766f},
+};
+const MxTileCost kGradF16[] = {
+    {32, 128, 7.15f, 2.77f, 0.568f, 1.11f, 1.27f},
+    {64, 128, 7.99f, 1.94f, 1.2f, 1.39f, 1.0f},
+    {128, 128, 8.13f, 2.9f, 1.68f, 2.31f, 1.02f},
+};
+const MxTileCost kGradF32[] = {
+    {32, 128, 6.87f, 4.18f, 0.343f, 1.16f, 1.0f},
+    {64, 128, 3.06f, 7.51f, 0.907f, 1.86f, 4.29f},
+    {128, 128, 7.26f, 4.54f, 1.05f, 2.97f, 1.03f},
+};
 
-// The direct kernels are for op 0; more than 32 rows of fp32, or two or three terms of 256 rows, do not fit the LDS.
-bool legal(const Tile& t, int op, dla_dtype dt) {
-  return t.n == kDirect ? op == 0 && (t.m <= 32 || dt != DLA_F32) : t.m < 256 || dt == DLA_BF16;
+struct Menu {
+  const MxTileCost* tiles;
+  int count;
+};
+template <int N>
+Menu menu(const MxTileCost (&t)[N]) {
+  return {t, N};
+}
+Menu menu_of(int op, dla_dtype dt) {
+  if (op == 0) return dt == DLA_F32 ? menu(kForwardF32) : dt == DLA_BF16 ? menu(kForwardBf16) : menu(kForwardF16);
+  return dt == DLA_F32 ? menu(kGradF32) : dt == DLA_BF16 ? menu(kGradBf16) : menu(kGradF16);
 }
 
 int64_t wide(int64_t terms) { return (terms + 63) / 64 * 64; }
@@ -142,33 +190,16 @@ int launch_to(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w, i
 }  // namespace
 
 int mx4_apply_menu(int op, dla_dtype dt, mx4_params* out, int cap) {
-  int count = 0;
-  for (const Tile& t : kTiles) {
-    if (!legal(t, op, dt)) continue;
-    if (out && count < cap) out[count] = mx4_params{t.m, t.n, 0};
-    ++count;
-  }
-  return count;
+  const Menu m = menu_of(op, dt);
+  for (int i = 0; i < m.count && i < cap && out; ++i) out[i] = mx4_params{m.tiles[i].m, m.tiles[i].n, 0};
+  return m.count;
 }
 
 int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const mx4_params* p, MxPlan* plan) {
-  MxPlan r = {0, 0, 0};
-  if (p) r = MxPlan{p->tile_m, p->tile_n, p->splits};
+  const Menu t = menu_of(op, dt);
   const int64_t terms = op == 0 ? k : n, out = op == 0 ? n : k;
-  if (r.tile_m < 0 || r.tile_n < 0 || r.splits < 0 || r.splits > kMaxSplits || r.splits > (terms + kMxStep - 1) / kMxStep) return DLA_ERR_UNSUPPORTED_PARAMS;
-  if (r.tile_m == 0 && r.tile_n == 0) {
-    const bool direct = op == 0 && m <= (dt == DLA_F32 ? 32 : 64);
-    r.tile_m = direct ? (int)(m + 15) / 16 * 16 : m <= 32 ? 32 : m <= 64 ? 64 : m < 1024 || dt != DLA_BF16 ? 128 : 256;
-    r.tile_n = direct ? kDirect : r.tile_m < 128 ? 128 : r.tile_m;
-  }
-  bool found = false;
-  for (const Tile& t : kTiles) found |= t.m == r.tile_m && t.n == r.tile_n && legal(t, op, dt);
-  if (!found) return DLA_ERR_UNSUPPORTED_PARAMS;
-  if (r.splits == 0) r.splits = 1;
-  const int64_t tiles = ((m + r.tile_m - 1) / r.tile_m) * ((out + r.tile_n - 1) / r.tile_n);
-  if (tiles * r.splits > 0x7fffffff || terms > kMxMaxLd / 2) return DLA_ERR_TOO_LARGE;
-  *plan = r;
-  return DLA_SUCCESS;
+  if (terms > kMxMaxLd / 2) return DLA_ERR_TOO_LARGE;
+  return mx4_choose(t.tiles, t.count, m, out, terms, p, plan);
 }
 
 size_t mx4_apply_bytes(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, int64_t n, int64_t k, const MxPlan& plan) {
