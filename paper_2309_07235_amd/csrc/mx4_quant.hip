@@ -5,16 +5,12 @@
 namespace dla {
 namespace {
 
+// Elements 0 .. valid - 1 of eight from p, the rest zero.  (One access of eight needs no more alignment than one element.)
 template <typename T>
-struct Run8 {  // eight elements as accesses of 16 bytes
-  typedef T type __attribute__((ext_vector_type(8)));
-};
-
-// Elements 0 .. valid - 1 of eight from p, the rest zero.  vec: p is aligned to 16 bytes.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int valid, bool vec, float* v) {
-  if (vec && valid >= 8) {
-    const typename Run8<T>::type r = *reinterpret_cast<const typename Run8<T>::type*>(p);
+__device__ __forceinline__ void load8(const T* p, int valid, float* v) {
+  typedef T run_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  if (valid >= 8) {
+    const run_t r = *reinterpret_cast<const run_t*>(p);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)r[i];
   } else {
@@ -56,7 +52,7 @@ __device__ __forceinline__ unsigned int max_of_four(unsigned int x) {
 
 // Along the rows: a lane takes eight neighbours, four lanes a block.
 template <typename T>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int per_row, bool vec,
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int per_row,
                                                             uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds) {
   const int64_t first = (int64_t)blockIdx.x * 256;
   const int64_t row0 = first / per_row;
@@ -66,88 +62,134 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* x, int64_t 
   if (row >= rows) return;
   float v[8];
   const int64_t left = cols - chunk * 8;
-  load8(x + row * ldx + chunk * 8, left > 8 ? 8 : (int)left, vec, v);
+  load8(x + row * ldx + chunk * 8, left > 8 ? 8 : (int)left, v);
   const unsigned int sc = scale_of(max_of_four(magnitude8(v)));
   *reinterpret_cast<unsigned int*>(q + row * ldq + chunk * 4) = elements8(v, sc);
   if ((threadIdx.x & 3) == 0) s[row * lds + (chunk >> 2)] = (uint8_t)sc;
 }
 
-// Across the rows, and along them too where q is given: a tile of 128 x 128 goes through LDS.  Its columns are rotated by 16
-// per 32 rows, so that 16 columns of four row blocks, which is what a wave reads at a time, lie in 64 banks.
+// Across the rows, and along them too where q is given, a tile of 128 x 128 a workgroup.  A wave takes 32 rows, which are one block of every column,
+// a lane 8 x 8 of them: everything that belongs to one block is in 4 lanes, neighbours for a row's block, 16 apart for a
+// column's.  What a lane has for a column is eight rows' elements, a dword; the columns' scales of the four waves meet in LDS.
 template <typename T>
-__global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int tiles_c, bool vec,
-                                                            uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds, uint8_t* qt, int64_t ldqt,
-                                                            uint8_t* st, int64_t ldst) {
-  __shared__ float tile[128 * 128];
+__global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int tiles_c, uint8_t* q, int64_t ldq,
+                                                            uint8_t* s, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* st, int64_t ldst) {
+  typedef T run_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  __shared__ unsigned int scales[128];
   const int64_t r0 = (int64_t)(blockIdx.x / (unsigned int)tiles_c) * 128, c0 = (int64_t)(blockIdx.x % (unsigned int)tiles_c) * 128;
-  const int tid = threadIdx.x, c = (tid & 15) * 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4;
+  const int64_t row = r0 + wave * 32 + group * 8, col = c0 + (lane & 15) * 8;
+  float v[8][8];
+  const T* const p = x + row * ldx + col;
+  if (r0 + 128 <= rows && c0 + 128 <= cols) {
+    run_t r[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = (tid >> 4) + 16 * i;
-    float v[8];
-    const int64_t left = r0 + r < rows ? cols - c0 - c : 0;
-    load8(x + (r0 + r) * ldx + c0 + c, left > 8 ? 8 : (int)left, vec, v);
-    const int at = r * 128 + ((c + 16 * (r >> 5)) & 127);
+    for (int i = 0; i < 8; ++i) r[i] = *reinterpret_cast<const run_t*>(p + i * ldx);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) tile[at + j] = v[j];
-    if (q) {
-      const unsigned int sc = scale_of(max_of_four(magnitude8(v)));
-      if (r0 + r < rows) {
-        *reinterpret_cast<unsigned int*>(q + (r0 + r) * ldq + (c0 + c) / 2) = elements8(v, sc);
-        if ((tid & 3) == 0) s[(r0 + r) * lds + (c0 + c) / 32] = (uint8_t)sc;
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = (float)r[i][j];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t left = row + i < rows ? cols - col : 0;
+      if (left >= 8) {
+        const run_t r = *reinterpret_cast<const run_t*>(p + i * ldx);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = (float)r[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = j < left ? (float)p[i * ldx + j] : 0.0f;
       }
     }
   }
-  __syncthreads();
-  const int lane = tid & 63, block = lane >> 4;
+  if (q) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int col = (tid >> 6) * 32 + i * 16 + (lane & 15);
-    float v[32];
-    const float* p = tile + block * 32 * 128 + ((col + 16 * block) & 127);
-#pragma unroll
-    for (int r = 0; r < 32; ++r) v[r] = p[r * 128];
-    const unsigned int sc = scale_of(max(max(magnitude8(v), magnitude8(v + 8)), max(magnitude8(v + 16), magnitude8(v + 24))));
-    if (c0 + col < cols) {
-      u32x4_t w;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = elements8(v + 8 * j, sc);
-      *reinterpret_cast<u32x4_t*>(qt + (c0 + col) * ldqt + r0 / 2 + block * 16) = w;
-      st[(c0 + col) * ldst + r0 / 32 + block] = (uint8_t)sc;
+    for (int i = 0; i < 8; ++i) {
+      const unsigned int sc = scale_of(max_of_four(magnitude8(v[i])));
+      const unsigned int w = elements8(v[i], sc);
+      if (row + i < rows) {
+        *reinterpret_cast<unsigned int*>(q + (row + i) * ldq + col / 2) = w;
+        if ((lane & 3) == 0) s[(row + i) * lds + col / 32] = (uint8_t)sc;
+      }
     }
   }
+  // the columns' largest magnitudes, two columns' halves put together at a time: in the end lane group g has columns of its own
+  unsigned int most[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    most[j] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most[j] = max(most[j], __float_as_uint(v[i][j]) & 0x7fffffffu);
+  }
+  unsigned int sc[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    unsigned int* const m = most + 4 * h;
+    swap_halves(m[0], m[2]);  // m[0]: columns 0 and 2 of the lower half's rows, m[2]: of the upper half's
+    swap_halves(m[1], m[3]);
+    unsigned int a = max(m[0], m[2]), b = max(m[1], m[3]);
+    swap_rows(a, b);          // a: groups 0, 2 hold column 0 and 2 of their even groups' rows, 1 and 3 column 1 and 3
+    const unsigned int own = scale_of(max(a, b));
+    // and back to all lanes: columns 0 and 2, 1 and 3, then each
+    unsigned int even = own, odd = own;
+    swap_rows(even, odd);
+    unsigned int c0l = even, c2l = even, c1l = odd, c3l = odd;
+    swap_halves(c0l, c2l);
+    swap_halves(c1l, c3l);
+    sc[4 * h] = c0l;
+    sc[4 * h + 1] = c1l;
+    sc[4 * h + 2] = c2l;
+    sc[4 * h + 3] = c3l;
+    reinterpret_cast<uint8_t*>(scales)[((lane & 15) * 8 + 4 * h + (group >> 1) * 2 + (group & 1)) * 4 + wave] = (uint8_t)own;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = v[i][j];
+    const unsigned int w = elements8(c, sc[j]);
+    if (col + j < cols) *reinterpret_cast<unsigned int*>(qt + (col + j) * ldqt + row / 2) = w;
+  }
+  __syncthreads();
+  if (threadIdx.x < 128 && c0 + threadIdx.x < cols) *reinterpret_cast<unsigned int*>(st + (c0 + threadIdx.x) * ldst + r0 / 32) = scales[threadIdx.x];
 }
 
+// A lane writes 16 bytes, of the elements of `per_row` such runs a row.
 template <typename T>
-__global__ void __launch_bounds__(256) dequantize_kernel(Mx4View w, int64_t cols, int per_row, bool vec, T* y, int64_t ldy) {
+__global__ void __launch_bounds__(256) dequantize_kernel(Mx4View w, int64_t cols, int per_row, T* y, int64_t ldy) {
+  constexpr int PER = 16 / (int)sizeof(T);
+  typedef T run_t __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
   const int64_t first = (int64_t)blockIdx.x * 256;
   const int64_t row0 = first / per_row;
   const unsigned int at = (unsigned int)(first - row0 * per_row) + threadIdx.x;
   const int64_t row = row0 + at / (unsigned int)per_row;
-  const int64_t chunk = at % (unsigned int)per_row;
+  const int64_t run = at % (unsigned int)per_row;
   if (row >= w.rows) return;
-  const unsigned int e = *reinterpret_cast<const unsigned int*>(w.q + row * w.ldq + chunk * 4);
-  const float sc = mx_scale(w.s[row * w.lds + (chunk >> 2)]);
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2_t p = i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 0)
-                       : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 1)
-                       : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 2)
-                                : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 3);
-    v[2 * i] = p[0];
-    v[2 * i + 1] = p[1];
+  unsigned int e;
+  if constexpr (PER == 8)
+    e = *reinterpret_cast<const unsigned int*>(w.q + row * w.ldq + run * 4);
+  else
+    e = *reinterpret_cast<const uint16_t*>(w.q + row * w.ldq + run * 2);
+  const float sc = mx_scale(w.s[row * w.lds + run * PER / 32]);
+  float2_t v[PER / 2];
+  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 0);
+  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 1);
+  if constexpr (PER == 8) {
+    v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 2);
+    v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 3);
   }
-  T* const out = y + row * ldy + chunk * 8;
-  const int64_t left = cols - chunk * 8;
-  if (vec && left >= 8) {
-    typename Run8<T>::type r;
+  T* const out = y + row * ldy + run * PER;
+  const int64_t left = cols - run * PER;
+  if (left >= PER) {
+    run_t r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (T)v[i];
-    *reinterpret_cast<typename Run8<T>::type*>(out) = r;
+    for (int i = 0; i < PER; ++i) r[i] = (T)v[i / 2][i % 2];
+    *reinterpret_cast<run_t*>(out) = r;
   } else {
-    for (int i = 0; i < 8; ++i)
-      if (i < left) out[i] = (T)v[i];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (i < left) out[i] = (T)v[i / 2][i % 2];
   }
 }
 
@@ -171,8 +213,6 @@ __global__ void __launch_bounds__(256) zero_kernel(T* c, int64_t ldc, int64_t to
   if (i < total) c[(i / n) * ldc + i % n] = (T)0.0f;
 }
 
-bool aligned16(const void* p, int64_t ld, int size) { return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0; }
-
 // Workgroups for `items`, or 0 where they are more than a launch can have.
 unsigned int grid_for(int64_t items, int64_t per_group) {
   const int64_t groups = (items + per_group - 1) / per_group;
@@ -182,28 +222,28 @@ unsigned int grid_for(int64_t items, int64_t per_group) {
 template <typename T>
 int quantize_typed(const T* x, int64_t ldx, int64_t rows, int64_t cols, uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds, uint8_t* qt,
                    int64_t ldqt, uint8_t* st, int64_t ldst, hipStream_t stream) {
-  const bool vec = aligned16(x, ldx, sizeof(T));
   if (qt) {
     const int64_t tiles_c = (cols + 127) / 128, tiles = tiles_c * ((rows + 127) / 128);
     const unsigned int grid = grid_for(tiles, 1);
     if (!grid) return DLA_ERR_TOO_LARGE;
-    hipLaunchKernelGGL(quantize_tile_kernel<T>, dim3(grid), dim3(256), 0, stream, x, ldx, rows, cols, (int)tiles_c, vec, q, ldq, s, lds, qt,
-                       ldqt, st, ldst);
+    hipLaunchKernelGGL(quantize_tile_kernel<T>, dim3(grid), dim3(256), 0, stream, x, ldx, rows, cols, (int)tiles_c, q, ldq, s, lds, qt, ldqt, st,
+                       ldst);
   } else {
     const int64_t per_row = (cols + kMxStep - 1) / kMxStep * (kMxStep / 8);
     const unsigned int grid = grid_for(rows * per_row, 256);
     if (!grid) return DLA_ERR_TOO_LARGE;
-    hipLaunchKernelGGL(quantize_rows_kernel<T>, dim3(grid), dim3(256), 0, stream, x, ldx, rows, cols, (int)per_row, vec, q, ldq, s, lds);
+    hipLaunchKernelGGL(quantize_rows_kernel<T>, dim3(grid), dim3(256), 0, stream, x, ldx, rows, cols, (int)per_row, q, ldq, s, lds);
   }
   return launch_status(__func__);
 }
 
 template <typename T>
 int dequantize_typed(const Mx4View& w, int64_t cols, T* y, int64_t ldy, hipStream_t stream) {
-  const int64_t per_row = (cols + 7) / 8;
+  constexpr int PER = 16 / (int)sizeof(T);
+  const int64_t per_row = (cols + PER - 1) / PER;
   const unsigned int grid = grid_for(w.rows * per_row, 256);
   if (!grid) return DLA_ERR_TOO_LARGE;
-  hipLaunchKernelGGL(dequantize_kernel<T>, dim3(grid), dim3(256), 0, stream, w, cols, (int)per_row, aligned16(y, ldy, sizeof(T)), y, ldy);
+  hipLaunchKernelGGL(dequantize_kernel<T>, dim3(grid), dim3(256), 0, stream, w, cols, (int)per_row, y, ldy);
   return launch_status(__func__);
 }
 
