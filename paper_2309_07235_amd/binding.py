@@ -402,15 +402,19 @@ class Mx4:
     __slots__ = ("q", "s", "rows", "cols", "_device", "_ldq", "_lds")
 
     def __init__(self, q, s, cols: int):
-        wide = mx4_padded(cols)
-        if q.dim() != 2 or s.dim() != 2 or q.dtype != torch.uint8 or s.dtype != torch.uint8 or s.shape[0] != q.shape[0]:
-            raise ValueError("Mx4: q and s must be uint8 matrices with the same number of rows")
-        if cols < 0 or q.shape[1] * 2 < wide or s.shape[1] * 32 < wide:
-            raise ValueError(f"Mx4: q and s must hold {wide} columns (mx4_padded({cols}))")
-        if s.device != q.device:
+        wide = -(-cols // 128) * 128
+        if q.dtype is not torch.uint8 or s.dtype is not torch.uint8 or q.dim() != 2 or s.dim() != 2:
+            raise ValueError("Mx4: q and s must be uint8 matrices")
+        (rows, per_q), (row_q, col_q), (rows_s, per_s), (row_s, col_s) = q.shape, q.stride(), s.shape, s.stride()
+        if rows_s != rows or cols < 0 or per_q * 2 < wide or per_s * 32 < wide:
+            raise ValueError(f"Mx4: q and s must have the same number of rows and hold {wide} columns (mx4_padded({cols}))")
+        if (col_q != 1 and per_q > 1) or (col_s != 1 and per_s > 1):
+            raise ValueError("Mx4: q and s must be row-major matrices (unit column stride)")
+        device = q.get_device()
+        if s.get_device() != device:
             raise ValueError("Mx4: q and s on different devices")
-        self.q, self.s, self.rows, self.cols, self._device = q, s, q.shape[0], int(cols), q.get_device()
-        self._ldq, self._lds = _leading(q, "q"), _leading(s, "s")
+        self.q, self.s, self.rows, self.cols, self._device = q, s, rows, cols, device
+        self._ldq, self._lds = (row_q if rows > 1 else per_q) or 1, (row_s if rows > 1 else per_s) or 1
 
     def _args(self):
         return self.q.data_ptr() or None, self._ldq, self.s.data_ptr() or None, self._lds
@@ -433,9 +437,9 @@ def mx4_padded(cols: int) -> int:
 
 def mx4_empty(rows: int, cols: int, device="cuda") -> Mx4:
     """Room for a microscaled matrix, to be filled by mx4_quantize."""
-    wide = mx4_padded(cols)
-    return Mx4(torch.empty((rows, wide // 2), dtype=torch.uint8, device=device),
-               torch.empty((rows, wide // 32), dtype=torch.uint8, device=device), cols)
+    steps = -(-cols // 128)
+    return Mx4(torch.empty((rows, steps * 64), dtype=torch.uint8, device=device),
+               torch.empty((rows, steps * 4), dtype=torch.uint8, device=device), cols)
 
 
 def _mx4_call(fn, name: str, stream, devices, args):
