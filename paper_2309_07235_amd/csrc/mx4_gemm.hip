@@ -20,7 +20,8 @@ constexpr int kNumTiles = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
 int steps_of(int64_t k) { return (int)((k + kMxStep - 1) / kMxStep); }
 
 // Eight waves a workgroup where there is one for each of the 256 units at most; four, so that two workgroups fit a unit's LDS, where
-// there are more (one row by 16384 x 4096 DIRECT_A us against DIRECT_B, by 8192 x 8192 DIRECT_C against DIRECT_D).
+// there are more (one row by 16384 x 4096, 512 workgroups: 8.6 us with four waves, 10.2 with eight; by 8192 x 8192, 256 workgroups
+// of eight waves: 9.1 us, by 8320 x 8192, 260 of four: 11.0).
 template <int MB, int D8, int D4>
 int launch_direct(const MxGemmArgs& g, hipStream_t stream) {
   const unsigned grid = (unsigned)(g.tiles_m * g.tiles_n * g.splits);
