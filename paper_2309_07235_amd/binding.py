@@ -414,7 +414,7 @@ class Mx4:
         if s.get_device() != device:
             raise ValueError("Mx4: q and s on different devices")
         self.q, self.s, self.rows, self.cols, self._device = q, s, rows, cols, device
-        self._ldq, self._lds = (row_q if rows > 1 else per_q) or 1, (row_s if rows > 1 else per_s) or 1
+        self._ldq, self._lds = (row_q, row_s) if rows > 1 else (per_q, per_s)
 
     def _args(self):
         return self.q.data_ptr() or None, self._ldq, self.s.data_ptr() or None, self._lds
@@ -427,7 +427,7 @@ def _leading(t, name: str) -> int:
     (rows, cols), (row, col) = t.shape, t.stride()
     if col != 1 and cols > 1:
         raise ValueError(f"{name} must be a row-major matrix (unit column stride)")
-    return (row if rows > 1 else cols) or 1
+    return row if rows > 1 else cols or 1  # (rows that share their memory: 0, refused by the call)
 
 
 def mx4_padded(cols: int) -> int:
@@ -495,6 +495,8 @@ def _mx4_workspace(need: int, device, workspace, stream):
             return None, None, 0, None
         with torch.cuda.stream(stream):  # memory of the stream that uses it (None: the current one)
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace.get_device()
 
 

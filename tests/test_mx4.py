@@ -149,3 +149,24 @@ def test_binding_refuses_shapes_and_types(B):
         B.mx4_dequantize(w, torch.zeros((4, 100)))
     with pytest.raises(TypeError):
         B.mx4_apply(0, torch.zeros((3, 100), dtype=torch.float64), w, torch.zeros((3, 4)))
+
+
+def test_rows_that_share_their_memory_are_refused(B):
+    """A broadcast matrix has row stride 0: one of one column would otherwise pass for a packed column."""
+    import torch
+    u8 = torch.uint8
+    one = torch.zeros((1, 1))
+    assert B._leading(one.expand(5, 1), "x") == 0 and B._leading(torch.zeros((1, 7)).expand(5, 7), "x") == 0
+    assert B._leading(one, "x") == 1 and B._leading(torch.zeros((0, 3)), "x") == 3 and B._leading(torch.zeros((1, 0)), "x") == 1
+    assert B.lib.mx4_quantize(FAKE, 0, 5, 1, B.DLA_F32, FAKE, 64, FAKE, 4, None, 0, None, 0, None) == -2
+    shared = B.Mx4(torch.zeros((1, 64), dtype=u8).expand(4, 64), torch.zeros((4, 4), dtype=u8), 100)
+    assert shared._args()[1] == 0
+    assert B.lib.mx4_dequantize(FAKE, 0, FAKE, 4, 4, 100, B.DLA_F32, FAKE, 100, None) == -2
+    with pytest.raises(ValueError):  # every other byte of a buffer
+        B._mx4_workspace(0, one.device, torch.zeros(512, dtype=u8)[::2], None)
+    with pytest.raises(ValueError):  # columns that are not neighbours
+        B.Mx4(torch.zeros((4, 128), dtype=u8)[:, ::2], torch.zeros((4, 4), dtype=u8), 100)
+    with pytest.raises(ValueError):
+        B.Mx4(torch.zeros((4, 64), dtype=torch.int8), torch.zeros((4, 4), dtype=u8), 100)
+    with pytest.raises(ValueError):
+        B.Mx4(torch.zeros((4, 64), dtype=u8), torch.zeros((3, 4), dtype=u8), 100)
