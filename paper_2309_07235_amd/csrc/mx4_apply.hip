@@ -114,19 +114,21 @@ int launch_direct(const MxApplyArgs& g, int tile_m, hipStream_t stream) {
 
 template <typename T>
 int launch_copy(const T* x, int64_t ldx, int64_t m, int64_t terms, int64_t to_ld, T* to, hipStream_t stream) {
-  const int64_t per_row = to_ld / 8, groups = (m * per_row + 255) / 256;
-  if (groups > 0x7fffffff) return DLA_ERR_TOO_LARGE;
-  hipLaunchKernelGGL(mx4_copy_kernel<T>, dim3((unsigned)groups), dim3(256), 0, stream, x, ldx, m, terms, (int)per_row, to);
+  const int64_t per_row = to_ld / 8;
+  const unsigned int groups = mx4_grid_for(m * per_row, 256);
+  if (!groups) return DLA_ERR_TOO_LARGE;
+  hipLaunchKernelGGL(mx4_copy_kernel<T>, dim3(groups), dim3(256), 0, stream, x, ldx, m, terms, (int)per_row, to);
   return launch_status(__func__);
 }
 
 template <dla_dtype DT>
 int launch_planes(const void* x, int64_t ldx, int64_t m, int64_t terms, void* planes, hipStream_t stream) {
   using T = typename MxType<DT>::type;
-  const int64_t per_row = wide(terms) / 8, groups = (m * per_row + 255) / 256;
-  if (groups > 0x7fffffff) return DLA_ERR_TOO_LARGE;
+  const int64_t per_row = wide(terms) / 8;
+  const unsigned int groups = mx4_grid_for(m * per_row, 256);
+  if (!groups) return DLA_ERR_TOO_LARGE;
   const bool vec = (uintptr_t)x % 16 == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
-  hipLaunchKernelGGL((mx4_planes_kernel<T, MxType<DT>::kTerms>), dim3((unsigned)groups), dim3(256), 0, stream, static_cast<const T*>(x), ldx, m, terms,
+  hipLaunchKernelGGL((mx4_planes_kernel<T, MxType<DT>::kTerms>), dim3(groups), dim3(256), 0, stream, static_cast<const T*>(x), ldx, m, terms,
                      (int)per_row, vec, static_cast<bf16x8_t*>(planes));
   return launch_status(__func__);
 }

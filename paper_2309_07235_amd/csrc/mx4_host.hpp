@@ -10,6 +10,12 @@ struct MxPlan {
   int tile_m, tile_n, splits;
 };
 
+// A launch has fewer than 2^32 threads; what needs more is refused.  Workgroups of 256 threads for `items`, or 0.
+inline unsigned int mx4_grid_for(int64_t items, int64_t per_group) {
+  const int64_t groups = (items + per_group - 1) / per_group;
+  return groups < (int64_t)1 << 24 ? (unsigned int)groups : 0;
+}
+
 int mx4_quantize_launch(const void* x, int64_t ldx, int64_t rows, int64_t cols, dla_dtype dt, uint8_t* q, int64_t ldq, uint8_t* s,
                         int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* st, int64_t ldst, hipStream_t stream);
 int mx4_dequantize_launch(const Mx4View& w, int64_t cols, dla_dtype dt, void* y, int64_t ldy, hipStream_t stream);

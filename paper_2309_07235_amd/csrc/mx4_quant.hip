@@ -213,24 +213,18 @@ __global__ void __launch_bounds__(256) zero_kernel(T* c, int64_t ldc, int64_t to
   if (i < total) c[(i / n) * ldc + i % n] = (T)0.0f;
 }
 
-// Workgroups for `items`, or 0 where they are more than a launch can have.
-unsigned int grid_for(int64_t items, int64_t per_group) {
-  const int64_t groups = (items + per_group - 1) / per_group;
-  return groups > 0x7fffffff ? 0u : (unsigned int)groups;
-}
-
 template <typename T>
 int quantize_typed(const T* x, int64_t ldx, int64_t rows, int64_t cols, uint8_t* q, int64_t ldq, uint8_t* s, int64_t lds, uint8_t* qt,
                    int64_t ldqt, uint8_t* st, int64_t ldst, hipStream_t stream) {
   if (qt) {
     const int64_t tiles_c = (cols + 127) / 128, tiles = tiles_c * ((rows + 127) / 128);
-    const unsigned int grid = grid_for(tiles, 1);
+    const unsigned int grid = mx4_grid_for(tiles, 1);
     if (!grid) return DLA_ERR_TOO_LARGE;
     hipLaunchKernelGGL(quantize_tile_kernel<T>, dim3(grid), dim3(256), 0, stream, x, ldx, rows, cols, (int)tiles_c, q, ldq, s, lds, qt, ldqt, st,
                        ldst);
   } else {
     const int64_t per_row = (cols + kMxStep - 1) / kMxStep * (kMxStep / 8);
-    const unsigned int grid = grid_for(rows * per_row, 256);
+    const unsigned int grid = mx4_grid_for(rows * per_row, 256);
     if (!grid) return DLA_ERR_TOO_LARGE;
     hipLaunchKernelGGL(quantize_rows_kernel<T>, dim3(grid), dim3(256), 0, stream, x, ldx, rows, cols, (int)per_row, q, ldq, s, lds);
   }
@@ -241,7 +235,7 @@ template <typename T>
 int dequantize_typed(const Mx4View& w, int64_t cols, T* y, int64_t ldy, hipStream_t stream) {
   constexpr int PER = 16 / (int)sizeof(T);
   const int64_t per_row = (cols + PER - 1) / PER;
-  const unsigned int grid = grid_for(w.rows * per_row, 256);
+  const unsigned int grid = mx4_grid_for(w.rows * per_row, 256);
   if (!grid) return DLA_ERR_TOO_LARGE;
   hipLaunchKernelGGL(dequantize_kernel<T>, dim3(grid), dim3(256), 0, stream, w, cols, (int)per_row, y, ldy);
   return launch_status(__func__);
@@ -250,7 +244,7 @@ int dequantize_typed(const Mx4View& w, int64_t cols, T* y, int64_t ldy, hipStrea
 template <typename T>
 int join_typed(const float* parts, int splits, int64_t m, int64_t n, T* c, int64_t ldc, bool onto, hipStream_t stream) {
   const int per = n % 4 == 0 ? 4 : 1;
-  const unsigned int grid = grid_for(m * n, 256 * per);
+  const unsigned int grid = mx4_grid_for(m * n, 256 * per);
   if (!grid) return DLA_ERR_TOO_LARGE;
   if (per == 4)
     hipLaunchKernelGGL((join_kernel<T, 4>), dim3(grid), dim3(256), 0, stream, parts, splits, m * n, n, c, ldc, onto);
@@ -261,7 +255,7 @@ int join_typed(const float* parts, int splits, int64_t m, int64_t n, T* c, int64
 
 template <typename T>
 int zero_typed(T* c, int64_t ldc, int64_t m, int64_t n, hipStream_t stream) {
-  const unsigned int grid = grid_for(m * n, 256);
+  const unsigned int grid = mx4_grid_for(m * n, 256);
   if (!grid) return DLA_ERR_TOO_LARGE;
   hipLaunchKernelGGL(zero_kernel<T>, dim3(grid), dim3(256), 0, stream, c, ldc, m * n, n);
   return launch_status(__func__);

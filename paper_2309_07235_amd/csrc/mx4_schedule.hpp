@@ -32,8 +32,11 @@ inline int mx4_choose(const MxTileCost* tiles, int count, int64_t rows, int64_t 
     const int64_t groups = ((rows + t.m - 1) / t.m) * ((cols + t.n - 1) / t.n);
     for (int s : kSplits) {
       if (r.splits) s = r.splits;
-      const bool fits = groups * s <= 0x7fffffff && (s == 1 || (double)rows * (double)cols * s <= (double)(1 << 26) || r.splits);
-      if (s <= steps && fits && (double)rows * (double)cols * s < 1e15) {
+      // (launches have fewer than 2^32 threads: up to 512 a tile here, one to an element where parts are joined; parts of more than
+      // 2^26 values are not chosen, but may be named)
+      const double values = (double)rows * (double)cols * s;
+      const bool fits = groups * s < (int64_t)1 << 23 && (s == 1 || (values < 4.0e9 * s && (r.splits || values <= (double)(1 << 26))));
+      if (s <= steps && fits) {
         const float each = (float)((groups * s + 255) / 256), n = (float)((steps + s - 1) / s);
         const float chain = t.first + t.step * n, work = each * (t.more + t.unit * n);
         float cost = t.start + (chain > work ? chain : work);

@@ -170,3 +170,25 @@ def test_rows_that_share_their_memory_are_refused(B):
         B.Mx4(torch.zeros((4, 64), dtype=torch.int8), torch.zeros((4, 4), dtype=u8), 100)
     with pytest.raises(ValueError):
         B.Mx4(torch.zeros((4, 64), dtype=u8), torch.zeros((3, 4), dtype=u8), 100)
+
+
+def test_launches_of_too_many_threads_are_refused(B):
+    """A launch has fewer than 2^32 threads.  (Without a GPU a call that gets as far as its launch fails with another code.)"""
+    big = 1 << 22
+    assert B.lib.mx4_quantize(FAKE, big, big, big, B.DLA_BF16, FAKE, big // 2, FAKE, big // 32, None, 0, None, 0, None) == B.DLA_ERR_TOO_LARGE
+    assert B.lib.mx4_quantize(FAKE, big, big, big, B.DLA_BF16, None, 0, None, 0, FAKE, big // 2, FAKE, big // 32, None) == B.DLA_ERR_TOO_LARGE
+    for dt in (B.DLA_F32, B.DLA_F16):
+        assert B.lib.mx4_dequantize(FAKE, 1 << 17, FAKE, 1 << 13, 1 << 18, 1 << 18, dt, FAKE, 1 << 18, None) == B.DLA_ERR_TOO_LARGE
+    n, one = 1 << 20, B.Mx4Params(16, 32, 1)
+    args = (FAKE, 64, FAKE, 4, FAKE, 64, FAKE, 4, FAKE, n, n, n, 128, B.DLA_BF16)
+    assert B.lib.mx4_gemm(0, *args, ctypes.byref(one), None, 0, None) == B.DLA_ERR_TOO_LARGE
+    two, m = B.Mx4Params(256, 256, 2), 1 << 18  # the tiles alone would do, joining their 2^36 values would not
+    args = (FAKE, 128, FAKE, 8, FAKE, 128, FAKE, 8, FAKE, m, m, m, 256, B.DLA_BF16)
+    assert B.lib.mx4_gemm(0, *args, ctypes.byref(two), FAKE, 1 << 60, None) == B.DLA_ERR_TOO_LARGE
+    assert B.lib.mx4_gemm(0, FAKE, 64, FAKE, 4, FAKE, 64, FAKE, 4, FAKE, n, n, n, 0, B.DLA_BF16, None, None, 0, None) == B.DLA_ERR_TOO_LARGE
+    wide = 1 << 21  # terms
+    many = 1 << 28
+    assert B.lib.mx4_apply(0, FAKE, wide, B.DLA_F32, FAKE, wide // 2, FAKE, wide // 32, FAKE, 1, B.DLA_F32, many, 1, wide, None, FAKE, 1 << 60,
+                           None) == B.DLA_ERR_TOO_LARGE
+    assert B.lib.mx4_apply(0, FAKE, 2 * wide, B.DLA_F32, FAKE, wide, FAKE, wide // 16, FAKE, 1, B.DLA_F32, 1, 1, 2 * wide, None, FAKE, 1 << 60,
+                           None) == B.DLA_ERR_TOO_LARGE
