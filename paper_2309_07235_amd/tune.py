@@ -14,11 +14,13 @@ Here the "code mold" is the library's pre-instantiated schedule menu, so an eval
   - `surrogate_search` Random-Forest surrogate on the parameter values, refitted after every evaluation,
                       next point = argmin over a candidate pool of  mean - kappa * std  (LCB);
   - `PerformanceDatabase`  every (configuration, runtime) pair, optionally mirrored to a CSV file;
-  - `mm3_problem`, `factor_problem`  the search spaces and timed objectives of the three kernels.
+  - `mm3_problem`, `factor_problem`  the search spaces and timed objectives of the three kernels;
+  - `mx4_problem`      the same of the microscaled products, `mx4_gemm` and `mx4_apply`.
 
 Nothing here is on the hot path; it only drives the C ABI through the Python binding.
 
   python -m paper_2309_07235_amd.tune --kernel mm3 --evals 100 --strategy rf --db mm3.csv
+  python -m paper_2309_07235_amd.tune --kernel mx4_apply --shape 48 8192 8192 --dtype f16 --evals 40 --from-default
 """
 from __future__ import annotations
 
@@ -170,7 +172,7 @@ def surrogate_search(space: SearchSpace, objective: Callable[[Dict[str, object]]
     return db
 
 
-# ------------------------------------------------------------------ the three kernels as tuning problems
+# ------------------------------------------------------------------ the kernels as tuning problems
 def _time_ms(fn, reps: int) -> float:
     """Median device time of fn() in ms (events on the current stream), after one untimed call."""
     import torch
@@ -254,11 +256,70 @@ def factor_problem(kind: str, n: int, seed: int = 5, reps: int = 3, dtype: str =
                               "defer_min_rows": d.defer_min_rows}
 
 
+MX4_MAX_PARTS = 1 << 31  # bytes of split sums that a search tries
+
+
+def mx4_space(kernel: str, op: int, m: int, n: int, k: int, dtype: str = "bf16"):
+    """Search space of a microscaled product: the tile (entry 0 = the library's own choice, the others = the menu's) and how many
+    workgroups share one along the sum; the library's default as a point of it."""
+    from . import binding as B
+
+    code = B.DLA_KERNEL_MX4_GEMM if kernel == "mx4_gemm" else B.DLA_KERNEL_MX4_APPLY
+    dt = {"f32": B.DLA_F32, "bf16": B.DLA_BF16, "f16": B.DLA_F16}[dtype]
+    terms, out = (n, k) if kernel == "mx4_apply" and op == 1 else (k, n)
+    d = B.mx4_default_params(code, op, m, n, k, dt)
+    tiles = [(0, 0)] + [(t.tile_m, t.tile_n) for t in B.mx4_enumerate_tiles(code, op, dt)]
+    most = min(32, -(-terms // 128))
+    splits = sorted({s for s in (1, 2, 3, 4, 6, 8, 12, 16, 24, 32) if s <= most} | {d.splits})
+    space = SearchSpace(["tile", "splits"], [tiles, splits], legal=lambda c: c["splits"] == 1 or c["splits"] * m * out * 4 <= MX4_MAX_PARTS)
+    return space, {"tile": (d.tile_m, d.tile_n), "splits": d.splits}
+
+
+def mx4_problem(kernel: str, op: int, m: int, n: int, k: int, seed: int = 6, reps: int = 5, dtype: str = "bf16"):
+    """Search space and objective of mx4_gemm (dtype: C's) or mx4_apply (X's and Y's); both operands of the one and the weights of
+    the other are normal values, microscaled on the device."""
+    import torch
+    from . import binding as B
+
+    space, default = mx4_space(kernel, op, m, n, k, dtype)
+    tdt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+
+    def normal(rows, cols):
+        return torch.randn((rows, cols), dtype=torch.float32, device="cuda", generator=gen).to(tdt)
+
+    def micro(rows, cols):
+        form = B.mx4_empty(rows, cols)
+        B.mx4_quantize(normal(rows, cols), form)
+        return form
+
+    w = micro(n, k)
+    if kernel == "mx4_gemm":
+        args = (op, micro(m, k), w, torch.zeros((m, n), dtype=tdt, device="cuda"))
+        fn = B.mx4_gemm
+    else:
+        args = (op, normal(m, n if op else k), w, torch.empty((m, k if op else n), dtype=tdt, device="cuda"))
+        fn = B.mx4_apply
+    room = {}  # the workspace of each schedule, kept for its timed calls
+
+    def objective(cfg):
+        p = B.Mx4Params(*cfg["tile"], cfg["splits"])
+        room.clear()
+        room["ws"] = fn(*args, p)
+        return _time_ms(lambda: fn(*args, p, workspace=room["ws"]), reps)
+
+    return space, objective, default
+
+
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser(description="search the exposed tile / block parameters of one kernel")
-    ap.add_argument("--kernel", choices=["mm3", "lu", "cholesky"], default="mm3")
+    ap.add_argument("--kernel", choices=["mm3", "lu", "cholesky", "mx4_gemm", "mx4_apply"], default="mm3")
     ap.add_argument("--n", type=int, default=4000, help="matrix size of the factorisations")
     ap.add_argument("--dataset", choices=["small", "extralarge"], default="extralarge", help="3mm shape")
+    ap.add_argument("--shape", type=int, nargs=3, metavar=("M", "N", "K"), default=[4096, 8192, 8192], help="sizes of mx4_gemm and mx4_apply")
+    ap.add_argument("--op", type=int, choices=[0, 1], default=0, help="their operation (see dla.h)")
+    ap.add_argument("--dtype", choices=["f32", "bf16", "f16"], default="bf16", help="the type of their ordinary matrices")
     ap.add_argument("--evals", type=int, default=100, help="evaluation budget (the paper uses 100)")
     ap.add_argument("--strategy", choices=["rf", "random"], default="rf")
     ap.add_argument("--seed", type=int, default=0)
@@ -273,6 +334,8 @@ def main(argv=None) -> int:
     if args.kernel == "mm3":
         dims = inputs.MM3_EXTRALARGE if args.dataset == "extralarge" else inputs.MM3_SMALL
         space, objective, default = mm3_problem(dims)
+    elif args.kernel.startswith("mx4_"):
+        space, objective, default = mx4_problem(args.kernel, args.op, *args.shape, dtype=args.dtype)
     else:
         space, objective, default = factor_problem("lu" if args.kernel == "lu" else "chol", args.n)
     db = PerformanceDatabase(space, args.db)

@@ -505,3 +505,20 @@ def test_offsets_past_32_bits(B):
     B.mx4_apply(0, x, w, z)
     xv, wv = f64(x), O.values(codes, scales)[:, :300]
     assert (np.abs(f64(z) - xv @ wv.T) <= bound(xv @ wv.T, np.abs(xv) @ np.abs(wv).T, 900, "float32")).all()
+
+
+@pytest.mark.parametrize("kernel,op,shape,dtype", [("mx4_gemm", 1, (70, 200, 900), "f32"), ("mx4_apply", 0, (9, 300, 700), "f16"),
+                                                   ("mx4_apply", 1, (40, 700, 130), "bf16")])
+def test_search_over_the_schedules(B, capsys, tmp_path, kernel, op, shape, dtype):
+    import json
+
+    from paper_2309_07235_amd import tune
+    announce(f"search {kernel} op {op} {shape} {dtype}")
+    db = tmp_path / "perf.csv"
+    assert tune.main(["--kernel", kernel, "--op", str(op), "--shape", *map(str, shape), "--dtype", dtype, "--evals", "8", "--strategy", "random",
+                      "--from-default", "--db", str(db)]) == 0
+    out = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    rows = db.read_text().strip().splitlines()
+    assert len(rows) == 9 and out["kernel"] == kernel and out["evaluations"] == 8
+    assert 0.0 < out["best_runtime_ms"] <= float(rows[1].split(",")[-2]) + 1e-3
+    assert len(out["best"]["tile"]) == 2 and out["best"]["splits"] >= 1

@@ -192,3 +192,41 @@ def test_launches_of_too_many_threads_are_refused(B):
                            None) == B.DLA_ERR_TOO_LARGE
     assert B.lib.mx4_apply(0, FAKE, 2 * wide, B.DLA_F32, FAKE, wide, FAKE, wide // 16, FAKE, 1, B.DLA_F32, 1, 1, 2 * wide, None, FAKE, 1 << 60,
                            None) == B.DLA_ERR_TOO_LARGE
+
+
+@pytest.mark.parametrize("kernel,op,m,n,k,dtype", [("mx4_gemm", 0, 100, 300, 5000, "f32"), ("mx4_gemm", 1, 8192, 8192, 8192, "bf16"),
+                                                   ("mx4_apply", 0, 1, 4096, 16384, "f16"), ("mx4_apply", 1, 333, 2200, 1801, "f32"),
+                                                   ("mx4_apply", 1, 5, 1, 200, "bf16")])
+def test_search_space_holds_the_default_and_legal_schedules_only(B, kernel, op, m, n, k, dtype):
+    from paper_2309_07235_amd import tune
+    space, default = tune.mx4_space(kernel, op, m, n, k, dtype)
+    assert space.decode(space.encode(default)) == default and space.is_legal(space.encode(default))
+    dt = {"f32": B.DLA_F32, "bf16": B.DLA_BF16, "f16": B.DLA_F16}[dtype]
+    out = B.Mx4Params()
+    for i in range(len(space.values[0])):
+        for j in range(len(space.values[1])):
+            if not space.is_legal((i, j)):
+                continue
+            c = space.decode((i, j))
+            p = B.Mx4Params(*c["tile"], c["splits"])
+            if kernel == "mx4_gemm":  # (a legal schedule's parts, or none)
+                need = B.lib.mx4_gemm_workspace_bytes(m, n, k, ctypes.byref(p))
+            else:
+                need = B.lib.mx4_apply_workspace_bytes(op, FAKE, n if op else k, dt, m, n, k, ctypes.byref(p))
+            parts = c["splits"] * m * (k if op and kernel == "mx4_apply" else n) * 4 if c["splits"] > 1 else 0
+            assert need >= parts, c
+    assert len(space.features(space.encode(default))) == 3
+
+
+def test_every_tile_is_the_choice_for_some_sizes(B):
+    """Nothing in the menus that no call without a schedule reaches."""
+    for kernel in (B.DLA_KERNEL_MX4_GEMM, B.DLA_KERNEL_MX4_APPLY):
+        for op in (0, 1) if kernel == B.DLA_KERNEL_MX4_APPLY else (0,):
+            for dt in (B.DLA_F32, B.DLA_BF16, B.DLA_F16):
+                left = {(t.tile_m, t.tile_n) for t in B.mx4_enumerate_tiles(kernel, op, dt)}
+                for m in (1, 2, 8, 16, 17, 24, 32, 33, 40, 48, 50, 64, 65, 96, 128, 200, 256, 400, 512, 700, 1024, 2048, 4096, 8192):
+                    for n in (64, 128, 256, 500, 1024, 2048, 4096, 8192, 16384):
+                        for k in (64, 128, 512, 1024, 2048, 4096, 8192):
+                            d = B.mx4_default_params(kernel, op, m, n, k, dt)
+                            left.discard((d.tile_m, d.tile_n))
+                assert not left, (kernel, op, dt, left)
