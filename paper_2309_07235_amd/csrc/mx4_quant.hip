@@ -193,18 +193,36 @@ __global__ void __launch_bounds__(256) dequantize_kernel(Mx4View w, int64_t cols
   }
 }
 
-// C = or += the sum of the parts, PER neighbours a thread (4 where the columns are a multiple of 4).
-template <typename T, int PER>
-__global__ void __launch_bounds__(256) join_kernel(const float* parts, int splits, int64_t total, int64_t n, T* c, int64_t ldc, bool onto) {
-  typedef float run_t __attribute__((ext_vector_type(PER)));
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * PER;
+// C = or += the sum of the parts, four neighbours a thread, which may lie in two rows.  (There are fewer than 2^32 values.)
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(const float* parts, int splits, unsigned int total, unsigned int n, T* c, int64_t ldc, bool onto) {
+  typedef float run_t __attribute__((ext_vector_type(4), aligned(4)));
+  const unsigned int i = (blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= total) return;
-  run_t sum = *reinterpret_cast<const run_t*>(parts + i);
+  run_t sum;
+  if (total - i >= 4) {
+    sum = *reinterpret_cast<const run_t*>(parts + i);
 #pragma unroll 4
-  for (int p = 1; p < splits; ++p) sum += *reinterpret_cast<const run_t*>(parts + p * total + i);
-  T* const out = c + (i / n) * ldc + i % n;
+    for (int p = 1; p < splits; ++p) sum += *reinterpret_cast<const run_t*>(parts + (int64_t)p * total + i);
+  } else {
 #pragma unroll
-  for (int v = 0; v < PER; ++v) out[v] = (T)(onto ? (float)out[v] + sum[v] : sum[v]);
+    for (int v = 0; v < 4; ++v) {
+      sum[v] = 0.0f;
+      for (int p = 0; v < (int)(total - i) && p < splits; ++p) sum[v] += parts[(int64_t)p * total + i + v];
+    }
+  }
+  unsigned int row = i / n, col = i - row * n;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    if (i + v < total) {
+      T* const out = c + (int64_t)row * ldc + col;
+      *out = (T)(onto ? (float)*out + sum[v] : sum[v]);
+    }
+    if (++col == n) {
+      col = 0;
+      ++row;
+    }
+  }
 }
 
 template <typename T>
@@ -243,13 +261,9 @@ int dequantize_typed(const Mx4View& w, int64_t cols, T* y, int64_t ldy, hipStrea
 
 template <typename T>
 int join_typed(const float* parts, int splits, int64_t m, int64_t n, T* c, int64_t ldc, bool onto, hipStream_t stream) {
-  const int per = n % 4 == 0 ? 4 : 1;
-  const unsigned int grid = mx4_grid_for(m * n, 256 * per);
+  const unsigned int grid = mx4_grid_for(m * n, 1024);
   if (!grid) return DLA_ERR_TOO_LARGE;
-  if (per == 4)
-    hipLaunchKernelGGL((join_kernel<T, 4>), dim3(grid), dim3(256), 0, stream, parts, splits, m * n, n, c, ldc, onto);
-  else
-    hipLaunchKernelGGL((join_kernel<T, 1>), dim3(grid), dim3(256), 0, stream, parts, splits, m * n, n, c, ldc, onto);
+  hipLaunchKernelGGL(join_kernel<T>, dim3(grid), dim3(256), 0, stream, parts, splits, (unsigned int)(m * n), (unsigned int)n, c, ldc, onto);
   return launch_status(__func__);
 }
 
