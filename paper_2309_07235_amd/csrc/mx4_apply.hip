@@ -7,7 +7,7 @@ namespace {
 
 constexpr int kDirect = 32;  // columns of a direct kernel's tile
 
-// The tiles.  The direct kernels are for op 0; more than 32 rows of fp32 there, and two or three terms of 256 rows, do not fit the LDS.  The
+// The tiles.  The direct kernels are for op 0; more than 16 rows of fp32 there, and two or three terms of 256 rows, do not fit the LDS.  The
 // costs are fitted to 3600 timings of 176 products (1 to 4096 rows, 128 to 8192 columns and terms, every tile, 1 to 32 splits): the choice takes
 // 1 to 6 % longer in the mean than the best of them, by operation and type.
 const MxTileCost kForwardBf16[] = {
@@ -31,7 +31,6 @@ const MxTileCost kForwardF16[] = {
 };
 const MxTileCost kForwardF32[] = {
     {16, 32, 2.32f, 7.07f, 0.0737f, 0.314f, 2.5f},
-    {32, 32, 3.73f, 5.31f, 0.22f, 0.551f, 2.97f},
     {32, 128, 7.17f, 3.88f, 0.306f, 0.865f, 1.0f},
     {64, 128, 3.56f, 6.08f, 1.14f, 1.44f, 4.25f},
     {128, 128, 7.93f, 2.94f, 0.508f, 2.63f, 1.0f},
@@ -73,41 +72,38 @@ bool whole(const void* x, int64_t ldx, dla_dtype dt, int64_t terms) {
   return dt == DLA_BF16 && (uintptr_t)x % 16 == 0 && ldx % 8 == 0 && terms % 64 == 0 && ldx <= kMxMaxLd / 2;
 }
 
-// X as the direct kernel takes it: aligned rows of whole steps (and offsets inside a tile of 64 rows in 32 bits).
-bool direct_takes(const void* x, int64_t ldx, int size, int64_t terms) {
-  return (uintptr_t)x % 16 == 0 && ldx * size % 16 == 0 && terms % kMxStep == 0 && ldx * size <= (int64_t)1 << 25;
+// X as the direct kernel takes it: 16-bit, aligned rows of whole steps (and offsets inside a tile of 64 rows in 32 bits).
+bool direct_takes(const void* x, int64_t ldx, dla_dtype dt, int64_t terms) {
+  return dt != DLA_F32 && (uintptr_t)x % 16 == 0 && ldx % 8 == 0 && terms % kMxStep == 0 && ldx <= (int64_t)1 << 24;
 }
 
 // The room for what a kernel reads instead of X.
 size_t copy_bytes(const MxPlan& plan, int64_t m, int64_t terms, dla_dtype dt) {
-  const int64_t count = plan.tile_n == kDirect ? (terms + kMxStep - 1) / kMxStep * kMxStep * (dt == DLA_F32 ? 4 : 2)
+  const int64_t count = plan.tile_n == kDirect ? (terms + kMxStep - 1) / kMxStep * kMxStep * 2 * (dt == DLA_F32 ? 3 : 1)
                                                : wide(terms) * 2 * (dt == DLA_F32 ? 3 : dt == DLA_F16 ? 2 : 1);
   return ((size_t)(m * count) + 255) / 256 * 256;
 }
 
-template <typename T, int MB, int XI, int WV, int DW>
+template <typename T, int TERMS, int MB, int XI, int WV, int DW>
 int launch_direct_as(const MxApplyArgs& g, hipStream_t stream) {
-  hipLaunchKernelGGL((mx4_apply_direct_kernel<T, MB, XI, WV, DW>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(WV * 64), 0, stream, g);
+  hipLaunchKernelGGL((mx4_apply_direct_kernel<T, TERMS, MB, XI, WV, DW>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(WV * 64), 0, stream, g);
   return launch_status(__func__);
 }
 
-// How many waves and how far ahead is what the LDS holds: of 16-bit rows up to 16, eight waves where there is one workgroup for each
-// of the 256 units at most, and four, so that two fit a unit, where there are more.  A load of X takes four rows of 16-bit
-// elements or two of fp32.
-template <typename T>
+// How many waves and how far ahead is what the LDS holds: up to 16 rows of 16 bits (4 of fp32), eight waves where there is one workgroup
+// for each of the 256 units at most, and four, so that several fit a unit, where there are more.
+template <typename T, int TERMS>
 int launch_direct(const MxApplyArgs& g, int tile_m, hipStream_t stream) {
-  if constexpr (sizeof(T) == 4) {
-    if (tile_m == 16) return g.m <= 2 ? launch_direct_as<T, 1, 1, 4, 4>(g, stream) : launch_direct_as<T, 1, 8, 4, 4>(g, stream);
-    return launch_direct_as<T, 2, 16, 4, 3>(g, stream);
+  const bool many = (int64_t)g.tiles_m * g.tiles_n * g.splits > 256;
+  if (tile_m == 16 && g.m <= 4) return many ? launch_direct_as<T, TERMS, 1, 1, 4, 4>(g, stream) : launch_direct_as<T, TERMS, 1, 1, 8, 4>(g, stream);
+  if constexpr (TERMS == 3) {
+    return launch_direct_as<T, TERMS, 1, 4, 4, 4>(g, stream);
   } else {
-    const bool many = (int64_t)g.tiles_m * g.tiles_n * g.splits > 256;
     switch (tile_m) {
-      case 16:
-        if (g.m <= 4) return many ? launch_direct_as<T, 1, 1, 4, 4>(g, stream) : launch_direct_as<T, 1, 1, 8, 4>(g, stream);
-        return many ? launch_direct_as<T, 1, 4, 4, 4>(g, stream) : launch_direct_as<T, 1, 4, 8, 4>(g, stream);
-      case 32: return launch_direct_as<T, 2, 8, 4, 6>(g, stream);
-      case 48: return launch_direct_as<T, 3, 12, 4, 6>(g, stream);
-      default: return launch_direct_as<T, 4, 16, 4, 3>(g, stream);
+      case 16: return many ? launch_direct_as<T, 1, 1, 4, 4, 4>(g, stream) : launch_direct_as<T, 1, 1, 4, 8, 4>(g, stream);
+      case 32: return launch_direct_as<T, 1, 2, 8, 4, 6>(g, stream);
+      case 48: return launch_direct_as<T, 1, 3, 12, 4, 6>(g, stream);
+      default: return launch_direct_as<T, 1, 4, 16, 4, 3>(g, stream);
     }
   }
 }
@@ -122,9 +118,9 @@ int launch_copy(const T* x, int64_t ldx, int64_t m, int64_t terms, int64_t to_ld
 }
 
 template <dla_dtype DT>
-int launch_planes(const void* x, int64_t ldx, int64_t m, int64_t terms, void* planes, hipStream_t stream) {
+int launch_planes(const void* x, int64_t ldx, int64_t m, int64_t terms, int64_t to_ld, void* planes, hipStream_t stream) {
   using T = typename MxType<DT>::type;
-  const int64_t per_row = wide(terms) / 8;
+  const int64_t per_row = to_ld / 8;
   const unsigned int groups = mx4_grid_for(m * per_row, 256);
   if (!groups) return DLA_ERR_TOO_LARGE;
   const bool vec = (uintptr_t)x % 16 == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
@@ -153,7 +149,7 @@ int launch_typed(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w
                        (int)(wide(terms) / 64), plan.splits, tiles_m, tiles_n};
   if (!whole(x, ldx, DT, terms)) {
     void* const planes = static_cast<char*>(workspace) + mx4_parts_bytes(m, out, plan);
-    const int rc = launch_planes<DT>(x, ldx, m, terms, planes, stream);
+    const int rc = launch_planes<DT>(x, ldx, m, terms, wide(terms), planes, stream);
     if (rc != DLA_SUCCESS) return rc;
     g.x = static_cast<const __bf16*>(planes);
     g.ldx = wide(terms);
@@ -172,17 +168,25 @@ int launch_to(int op, const void* x, int64_t ldx, int64_t m, const Mx4View& w, i
               void* workspace, hipStream_t stream) {
   using T = typename MxType<DT>::type;
   if (plan.tile_n == kDirect) {
-    const int64_t steps = (k + kMxStep - 1) / kMxStep;
-    MxApplyArgs g = {x, w, y, static_cast<float*>(workspace), ldx, ldy, (int)m, (int)steps, plan.splits, (int)((m + plan.tile_m - 1) / plan.tile_m),
+    const int64_t steps = (k + kMxStep - 1) / kMxStep, to_ld = steps * kMxStep;
+    MxApplyArgs g = {x, w, y, static_cast<float*>(workspace), ldx, 0, ldy, (int)m, (int)steps, plan.splits, (int)((m + plan.tile_m - 1) / plan.tile_m),
                      (w.rows + kDirect - 1) / kDirect, dt_y};
-    if (!direct_takes(x, ldx, sizeof(T), k)) {
-      T* const to = reinterpret_cast<T*>(static_cast<char*>(workspace) + mx4_parts_bytes(m, w.rows, plan));
-      const int rc = launch_copy<T>(static_cast<const T*>(x), ldx, m, k, steps * kMxStep, to, stream);
+    if (!direct_takes(x, ldx, DT, k)) {
+      void* const to = static_cast<char*>(workspace) + mx4_parts_bytes(m, w.rows, plan);
+      int rc;
+      if constexpr (DT == DLA_F32)
+        rc = launch_planes<DT>(x, ldx, m, k, to_ld, to, stream);
+      else
+        rc = launch_copy<T>(static_cast<const T*>(x), ldx, m, k, to_ld, static_cast<T*>(to), stream);
       if (rc != DLA_SUCCESS) return rc;
       g.x = to;
-      g.ldx = steps * kMxStep;
+      g.ldx = to_ld;
+      g.plane = m * to_ld;
     }
-    return launch_direct<T>(g, plan.tile_m, stream);
+    if constexpr (DT == DLA_F32)
+      return launch_direct<__bf16, 3>(g, plan.tile_m, stream);
+    else
+      return launch_direct<T, 1>(g, plan.tile_m, stream);
   }
   if (dt_y == DLA_F32) return launch_typed<DT, float>(op, x, ldx, m, w, k, y, ldy, plan, workspace, stream);
   if (dt_y == DLA_BF16) return launch_typed<DT, __bf16>(op, x, ldx, m, w, k, y, ldy, plan, workspace, stream);
@@ -206,7 +210,7 @@ int mx4_apply_plan(int op, int64_t m, int64_t n, int64_t k, dla_dtype dt, const 
 
 size_t mx4_apply_bytes(int op, const void* x, int64_t ldx, dla_dtype dt, int64_t m, int64_t n, int64_t k, const MxPlan& plan) {
   const int64_t terms = op == 0 ? k : n;
-  const bool as_it_is = plan.tile_n == kDirect ? direct_takes(x, ldx, dt == DLA_F32 ? 4 : 2, terms) : whole(x, ldx, dt, terms);
+  const bool as_it_is = plan.tile_n == kDirect ? direct_takes(x, ldx, dt, terms) : whole(x, ldx, dt, terms);
   return mx4_parts_bytes(m, op == 0 ? n : k, plan) + (as_it_is ? 0 : copy_bytes(plan, m, terms, dt));
 }
 

@@ -6,11 +6,11 @@
 namespace dla {
 
 struct MxApplyArgs {
-  const void* x;         // rows aligned to 16 bytes, whole steps of 128 terms
+  const void* x;         // rows aligned to 16 bytes, whole steps of 128 terms; planes of bf16 terms, `plane` elements apart
   Mx4View w;
   void* y;
   float* parts;
-  int64_t ldx, ldy;
+  int64_t ldx, plane, ldy;
   int m, steps;          // Y m x w.rows, steps of 128 terms
   int splits, tiles_m, tiles_n;
   dla_dtype dt_y;
@@ -42,37 +42,20 @@ __device__ __forceinline__ void mx_terms_of(T __attribute__((ext_vector_type(8))
 // steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X two.  Through LDS, because the matrix instructions
 // want neighbouring lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16 (4096 x 16384 weights,
 // one row, bf16: 16 us with loads to registers).
-//   bf16, fp32   a lane's block of W is made bf16 with its scale, X is one or three terms; instruction b takes eight elements of
-//                every lane's block;
+//   bf16, fp32   a lane's block of W is made bf16 with its scale; X is one plane of bf16 or, for fp32, three that add up to it (made by a
+//                launch in front: made here, by every workgroup, they cost more than the rest of the call); instruction b takes
+//                eight elements of every lane's block;
 //   fp16         lanes exchange dwords so that instruction b takes block b, whose elements are made fp16 without the scale (with it
 //                they would leave the type's range); the sum is scaled on its way to the running one, in fp32.
-// XI: loads of X a step, fewer than its MB * 16 rows would take where only the first rows exist; what the others hold in LDS reaches rows
-// of the result that are not stored.
-template <typename T>
-struct MxOperand {
-  static constexpr int kTerms = 3;
-  typedef bf16x8_t type;
-};
-template <>
-struct MxOperand<__bf16> {
-  static constexpr int kTerms = 1;
-  typedef bf16x8_t type;
-};
-template <>
-struct MxOperand<_Float16> {
-  static constexpr int kTerms = 1;
-  typedef f16x8_t type;
-};
-
-template <typename T, int MB, int XI, int WV, int DW>
+// XI: loads of X a plane and step, of four rows each: one where there are at most four rows, whose place the others of the instruction read
+// too (they reach rows of the result that are not stored).
+template <typename T, int TERMS, int MB, int XI, int WV, int DW>
 __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g) {
-  constexpr int NB = 2, TM = MB * 16, TN = NB * 16, TERMS = MxOperand<T>::kTerms;
+  constexpr int NB = 2, TM = MB * 16, TN = NB * 16, XR = XI * 4;
   constexpr bool F16 = std::is_same<T, _Float16>::value;
-  constexpr int XCH = kMxStep * (int)sizeof(T) / 16, RPI = 64 / XCH;   // 16-byte chunks of a row and step; rows a load fills
-  constexpr int PER = 8 * (int)sizeof(T) / 16;                         // chunks of eight elements
-  constexpr int W_RING = DW * NB * 64, X_STAGE = TM * XCH, RING = W_RING + 2 * X_STAGE + 2 * TN;  // units of 16 bytes
+  static_assert(sizeof(T) == 2 && (XR == TM || XR == 4) && (!F16 || TERMS == 1), "rows of 256 bytes a step, all of them or four");
+  constexpr int W_RING = DW * NB * 64, X_STAGE = TERMS * XR * 16, RING = W_RING + 2 * X_STAGE + 2 * TN;  // units of 16 bytes
   static_assert(WV * RING * 16 <= 160 * 1024 && RING * 16 >= TM * TN * 4, "LDS");
-  using V = typename MxOperand<T>::type;
   typedef T run_t __attribute__((ext_vector_type(8)));
   __shared__ u32x4_t lds[WV * RING];
   const int tiles = g.tiles_m * g.tiles_n;
@@ -85,7 +68,7 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
   u32x4_t* const ring = lds + wave * RING;
   const unsigned int at_w = lds_offset(ring), at_x = at_w + W_RING * 16, at_s = at_x + 2 * X_STAGE * 16;
 
-  // W: a load fills 16 rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4; X: RPI rows, chunk c of row r at c ^ r % 16
+  // W: a load fills 16 rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4; X: 4 rows of 256 bytes, chunk c of row r at c ^ r % 16
   const uint8_t* const wq = g.w.q + (int64_t)n0 * g.w.ldq;
   const uint8_t* const ws = g.w.s + (int64_t)n0 * g.w.lds;
   const T* const x = static_cast<const T*>(g.x) + (int64_t)m0 * g.ldx;
@@ -95,8 +78,8 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
     woff[j] = (unsigned int)(min(j * 16 + lane / 4, g.w.rows - 1 - n0) * (int)g.w.ldq) + ((lane & 3) ^ (lane >> 4)) * 16;
 #pragma unroll
   for (int i = 0; i < XI; ++i) {
-    const int r = i * RPI + lane / XCH;
-    xoff[i] = (unsigned int)min(r, g.m - 1 - m0) * (unsigned int)(g.ldx * (int)sizeof(T)) + ((lane % XCH) ^ (r & 15)) * 16;
+    const int r = i * 4 + lane / 16;
+    xoff[i] = (unsigned int)min(r, g.m - 1 - m0) * (unsigned int)(g.ldx * 2) + ((lane & 15) ^ (r & 15)) * 16;
   }
   const unsigned int soff = (unsigned int)(min(lane & 31, g.w.rows - 1 - n0) * (int)g.w.lds);
   // (loads past the end repeat its last step, so that their number in flight is always the same)
@@ -108,7 +91,9 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
   auto load_x = [&](int s, int slot) {
     const T* const from = x + (int64_t)min(s, end - 1) * kMxStep;
 #pragma unroll
-    for (int i = 0; i < XI; ++i) load_to_lds(from, xoff[i], at_x + slot * X_STAGE * 16 + i * 1024);
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int i = 0; i < XI; ++i) load_to_lds(from + t * g.plane, xoff[i], at_x + slot * X_STAGE * 16 + (t * XI + i) * 1024);
   };
   // the scales of four steps, 16 bytes a row, moved back to begin at most four steps before the row's end
   auto scales_from = [&](int chunk) { return min(begin + chunk * 4, g.steps - 4); };
@@ -140,7 +125,7 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
     int slot = 0;
     for (int s = begin; s < end; ++s) {
       const int i = s - begin, chunk = i >> 2;
-      wait_loads<NB + XI>();  // this step has arrived: only the next one's loads of X, and W's beside them, are younger
+      wait_loads<NB + TERMS * XI>();  // this step has arrived: only the next one's loads of X, and W's beside them, are younger
       const u32x4_t* const wr = ring + slot * NB * 64;
       const u32x4_t* const xr = ring + W_RING + (i & 1) * X_STAGE;
       const unsigned int* const sr = reinterpret_cast<const unsigned int*>(ring + W_RING + 2 * X_STAGE + (chunk & 1) * TN) + (g.steps >= 4 ? s - scales_from(chunk) : i);
@@ -152,20 +137,16 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
         for (int b = 0; b < 4; ++b) w[j][b] = q[b];
         sc[j] = sr[(j * 16 + l15) * 4];
       }
-      run_t xv[4][MB];
+      run_t xv[4][TERMS][MB];
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int k = 0; k < MB; ++k) {
-          const int r = k * 16 + l15, c = (F16 ? b * 4 + l4 : l4 * 4 + b) * PER;
-          union {
-            u32x4_t u[PER];
-            run_t v;
-          } o;
+        for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-          for (int p = 0; p < PER; ++p) o.u[p] = xr[r * XCH + ((c + p) ^ l15)];
-          xv[b][k] = o.v;
-        }
+          for (int k = 0; k < MB; ++k) {
+            const int r = XR < 16 ? l15 & (XR - 1) : k * 16 + l15, c = F16 ? b * 4 + l4 : l4 * 4 + b;
+            xv[b][t][k] = __builtin_bit_cast(run_t, xr[(t * XR + r) * 16 + (c ^ (r & 15))]);
+          }
       wait_lds();  // (before what was read is overwritten)
       if ((i & 3) == 0 && s + 4 < end) load_s(chunk + 1);
       load_w(s + DW, slot);
@@ -186,31 +167,23 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
       }
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        V xt[MB][TERMS];
-#pragma unroll
-        for (int k = 0; k < MB; ++k) {
-          if constexpr (F16)
-            xt[k][0] = xv[b][k];
-          else
-            mx_terms_of<T, TERMS>(xv[b][k], xt[k]);
-        }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
           if constexpr (F16) {
-            const V wv = mx_values_f16(w[j][b]);
+            const f16x8_t wv = mx_values_f16(w[j][b]);
             const float f = mx_scale_value(sc[j] >> (8 * b));
 #pragma unroll
             for (int k = 0; k < MB; ++k) {
-              const float4_t sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(xt[k][0], wv, float4_t{0, 0, 0, 0}, 0, 0, 0);
+              const float4_t sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[b][0][k], wv, float4_t{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
               for (int v = 0; v < 4; ++v) acc[k][j][v] = __builtin_fmaf(sum[v], f, acc[k][j][v]);
             }
           } else {
-            const V wv = mx_values(w[j][b], own[j]);
+            const bf16x8_t wv = mx_values(w[j][b], own[j]);
 #pragma unroll
             for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
-              for (int k = 0; k < MB; ++k) acc[k][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xt[k][t], wv, acc[k][j], 0, 0, 0);
+              for (int k = 0; k < MB; ++k) acc[k][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[b][t][k], wv, acc[k][j], 0, 0, 0);
           }
         }
       }
