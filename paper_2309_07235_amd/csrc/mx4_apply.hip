@@ -8,7 +8,7 @@ namespace {
 constexpr int kDirect = 32;  // columns of a direct kernel's tile
 
 // The tiles.  The direct kernels are for op 0; more than 16 rows of fp32 there, and two or three terms of 256 rows, do not fit the LDS.  The
-// costs are fitted to 3600 timings of 176 products (1 to 4096 rows, 128 to 8192 columns and terms, every tile, 1 to 32 splits): the choice takes
+// costs are fitted to 4000 timings of 190 products (1 to 4096 rows, 128 to 8192 columns and terms, every tile, 1 to 32 splits): the choice takes
 // 1 to 6 % longer in the mean than the best of them, by operation and type.
 const MxTileCost kForwardBf16[] = {
     {16, 32, 7.02f, 2.86f, 0.0348f, 0.0982f, 0.702f},
@@ -30,10 +30,10 @@ const MxTileCost kForwardF16[] = {
     {128, 128, 2.83f, 8.18f, 1.61f, 0.5f, 0.994f},
 };
 const MxTileCost kForwardF32[] = {
-    {16, 32, 2.32f, 7.07f, 0.0737f, 0.314f, 2.5f},
-    {32, 128, 7.17f, 3.88f, 0.306f, 0.865f, 1.0f},
-    {64, 128, 3.56f, 6.08f, 1.14f, 1.44f, 4.25f},
-    {128, 128, 7.93f, 2.94f, 0.508f, 2.63f, 1.0f},
+    {16, 32, 3.15f, 8.18f, 0.0402f, 0.198f, 2.19f},
+    {32, 128, 8.07f, 2.88f, 0.262f, 0.742f, 0.683f},
+    {64, 128, 5.85f, 4.54f, 0.841f, 1.32f, 2.73f},
+    {128, 128, 6.45f, 3.0f, 0.5f, 2.32f, 3.31f},
 };
 const MxTileCost kGradBf16[] = {
     {32, 128, 5.51f, 2.2f, 0.862f, 0.748f, 1.01f},
