@@ -301,7 +301,7 @@ int dla_rank_update(int lower, const void* d_l, const void* d_r, void* d_c, int6
  * The columns are padded to a multiple of 128, P = mx4_padded(cols): rows hold P / 2 and P / 32 bytes, and the padding has to be
  * zero in both arrays, as mx4_quantize leaves it (the products run over it).  q and ldq are multiples of 16, s and lds of
  * 4 (bytes); ldq >= P / 2, lds >= P / 32, both at most 2^22 (a longer row is refused with DLA_ERR_TOO_LARGE, as is what one
- * launch cannot do: conversions of 2^34 elements and more, and products of 2^22 tiles and more, may be).
+ * launch cannot do: conversions of 2^34 elements and more, and products of 2^22 tiles and more, can be).
  * Outputs must not overlap inputs or each other.
  */
 int64_t mx4_padded(int64_t cols); /* cols rounded up to a multiple of 128; 0 for a negative one */

@@ -70,11 +70,12 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* x, int64_t 
 
 // Across the rows, and along them too where q is given, a tile of 128 x 128 a workgroup.  A wave takes 32 rows, which are one block of every column,
 // a lane 8 x 8 of them: everything that belongs to one block is in 4 lanes, neighbours for a row's block, 16 apart for a
-// column's.  What a lane has for a column is eight rows' elements, a dword; the columns' scales of the four waves meet in LDS.
+// column's.  What a lane has for a column is eight rows' elements, a dword; they and the scales of the four waves meet in LDS.
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int tiles_c, uint8_t* q, int64_t ldq,
                                                             uint8_t* s, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* st, int64_t ldst) {
   typedef T run_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  __shared__ u32x4_t turned[128 * 4];
   __shared__ unsigned int scales[128];
   const int64_t r0 = (int64_t)(blockIdx.x / (unsigned int)tiles_c) * 128, c0 = (int64_t)(blockIdx.x % (unsigned int)tiles_c) * 128;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4;
@@ -143,52 +144,51 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t 
     sc[4 * h + 3] = c3l;
     reinterpret_cast<uint8_t*>(scales)[((lane & 15) * 8 + 4 * h + (group >> 1) * 2 + (group & 1)) * 4 + wave] = (uint8_t)own;
   }
+  // A column's 64 bytes are put together in LDS: column 8 l + j at slot 16 j + l, wave w's 16 bytes of it at chunk w ^ l / 4, so that what
+  // a wave writes and reads at a time lies in all banks.
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = v[i][j];
-    const unsigned int w = elements8(c, sc[j]);
-    if (col + j < cols) *reinterpret_cast<unsigned int*>(qt + (col + j) * ldqt + row / 2) = w;
+    reinterpret_cast<unsigned int*>(turned + (j * 16 + (lane & 15)) * 4 + (wave ^ (lane >> 2 & 3)))[group] = elements8(c, sc[j]);
   }
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int slot = (threadIdx.x >> 2) + 64 * i, w = threadIdx.x & 3, l = slot & 15, c = l * 8 + (slot >> 4);
+    if (c0 + c < cols) *reinterpret_cast<u32x4_t*>(qt + (c0 + c) * ldqt + r0 / 2 + w * 16) = turned[slot * 4 + (w ^ (l >> 2))];
+  }
   if (threadIdx.x < 128 && c0 + threadIdx.x < cols) *reinterpret_cast<unsigned int*>(st + (c0 + threadIdx.x) * ldst + r0 / 32) = scales[threadIdx.x];
 }
 
-// A lane writes 16 bytes, of the elements of `per_row` such runs a row.
+// A lane takes eight neighbours; there are `per_row` such runs a row.
 template <typename T>
 __global__ void __launch_bounds__(256) dequantize_kernel(Mx4View w, int64_t cols, int per_row, T* y, int64_t ldy) {
-  constexpr int PER = 16 / (int)sizeof(T);
-  typedef T run_t __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+  typedef T run_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   const int64_t first = (int64_t)blockIdx.x * 256;
   const int64_t row0 = first / per_row;
   const unsigned int at = (unsigned int)(first - row0 * per_row) + threadIdx.x;
   const int64_t row = row0 + at / (unsigned int)per_row;
   const int64_t run = at % (unsigned int)per_row;
   if (row >= w.rows) return;
-  unsigned int e;
-  if constexpr (PER == 8)
-    e = *reinterpret_cast<const unsigned int*>(w.q + row * w.ldq + run * 4);
-  else
-    e = *reinterpret_cast<const uint16_t*>(w.q + row * w.ldq + run * 2);
-  const float sc = mx_scale(w.s[row * w.lds + run * PER / 32]);
-  float2_t v[PER / 2];
+  const unsigned int e = *reinterpret_cast<const unsigned int*>(w.q + row * w.ldq + run * 4);
+  const float sc = mx_scale(w.s[row * w.lds + (run >> 2)]);
+  float2_t v[4];
   v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 0);
   v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 1);
-  if constexpr (PER == 8) {
-    v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 2);
-    v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 3);
-  }
-  T* const out = y + row * ldy + run * PER;
-  const int64_t left = cols - run * PER;
-  if (left >= PER) {
+  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 2);
+  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, sc, 3);
+  T* const out = y + row * ldy + run * 8;
+  const int64_t left = cols - run * 8;
+  if (left >= 8) {
     run_t r;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) r[i] = (T)v[i / 2][i % 2];
+    for (int i = 0; i < 8; ++i) r[i] = (T)v[i / 2][i % 2];
     *reinterpret_cast<run_t*>(out) = r;
   } else {
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < 8; ++i)
       if (i < left) out[i] = (T)v[i / 2][i % 2];
   }
 }
@@ -251,8 +251,7 @@ int quantize_typed(const T* x, int64_t ldx, int64_t rows, int64_t cols, uint8_t*
 
 template <typename T>
 int dequantize_typed(const Mx4View& w, int64_t cols, T* y, int64_t ldy, hipStream_t stream) {
-  constexpr int PER = 16 / (int)sizeof(T);
-  const int64_t per_row = (cols + PER - 1) / PER;
+  const int64_t per_row = (cols + 7) / 8;
   const unsigned int grid = mx4_grid_for(w.rows * per_row, 256);
   if (!grid) return DLA_ERR_TOO_LARGE;
   hipLaunchKernelGGL(dequantize_kernel<T>, dim3(grid), dim3(256), 0, stream, w, cols, (int)per_row, y, ldy);
