@@ -138,7 +138,6 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
   constexpr int STAGE = (TM + TN) * 4;               // a step's rows of both operands, in units of 16 bytes
   __shared__ u32x4_t rows[4 * STAGE];
   __shared__ u32x4_t scales[2][TM + TN];             // those of four steps at a time, 16 bytes a row
-  __shared__ u32x4_t unread[WM * WN * 64];
   const int tiles = g.tiles_m * g.tiles_n;
   const int split = (int)blockIdx.x / tiles;
   int ti, tj;
@@ -249,19 +248,6 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
   load(1, 1);
   load(2, 2);
   load(3, 3);
-  // What is added to is fetched too, as far as an XCD's L2 (4 MB for 32 workgroups): its lines go to LDS that nobody reads.  C += A*B^T of
-  // 1600 x 1800, k = 2000, C not in a cache: fp32 21 us without, 19 with, bf16 18.6 and 15.7; 8192 x 8192, k = 1024, bf16 184 and 135.
-  constexpr int PER = 16 / (int)sizeof(T), RPL = 64 * PER / TN, LC = TM / RPL / (WM * WN);
-  static_assert(RPL * LC * WM * WN == TM && LC + 4 * L + 1 < 64, "whole loads, all of them counted");
-  if (TM * TN * sizeof(T) <= 131072 && g.onto && g.splits == 1 && (uintptr_t)g.c % 16 == 0 && g.ldc % PER == 0 && g.ldc <= kMxMaxLd && g.b.rows >= PER) {
-    const unsigned int to = lds_offset(unread) + wave * 1024;
-    const int col = min(n0 + lane % (TN / PER) * PER, g.b.rows / PER * PER - PER);
-#pragma unroll 1
-    for (int i = 0; i < LC; ++i) {
-      const int row = min(m0 + (wave * LC + i) * RPL + lane / (TN / PER), g.a.rows - 1) - m0;
-      load_to_lds(static_cast<const T*>(g.c) + (int64_t)m0 * g.ldc, ((unsigned int)row * (unsigned int)g.ldc + (unsigned int)col) * (unsigned int)sizeof(T), to);
-    }
-  }
   wait_loads_and_barrier<3 * L>();
   Half x = read(0, 0);
   Scales w = read_scales(0);

@@ -65,7 +65,7 @@ __device__ __forceinline__ void mx_store_tile(u32x4_t* lds, const f32x16_t (&acc
   typedef T out_t __attribute__((ext_vector_type(PER)));
   typedef S quad_t __attribute__((ext_vector_type(4)));
   const int l31 = lane & 31, l5 = lane >> 5;
-  const bool vec = (uintptr_t)c % sizeof(out_t) == 0 && ldc % PER == 0;
+  const bool vec = (uintptr_t)c % sizeof(out_t) == 0 && ldc % PER == 0 && cols >= PER;
   // chunk c of a row lies at c ^ (r / RPB) % CH: a wave's accesses take all banks
   auto place = [&](int r, int chunk) { return r * CH + (chunk ^ ((r / RPB) & (CH - 1))); };
   auto in_order = [] {  // what other lanes of the wave have written
@@ -89,18 +89,18 @@ __device__ __forceinline__ void mx_store_tile(u32x4_t* lds, const f32x16_t (&acc
         }
     in_order();
     const int first = c0 + p * WIDE;
-    // A lane's N accesses, U at a time so that U loads of what is added to are on their way: as many as the registers hold beside the
-    // sums (at most one in the largest tile where those are 16 bytes, else the sums spill: 8192 x 8192 fp32, k = 1024, 263 us for 198).
-    constexpr int N = R * CH / 64, MOST = R * C > 4096 ? (sizeof(out_t) == 16 ? 1 : 4) : 8, U = N < MOST ? N : MOST;
+    // A lane's N accesses, U at a time so that U loads of what is added to are on their way, without a branch around each (C += A*B^T,
+    // 1600 x 1800, k = 2000, fp32, the largest part of it: 21 us with branches, 16 without): as many as the registers hold.
+    constexpr int N = R * CH / 64, MOST = R * C > 4096 ? 4 : 128 / (int)sizeof(out_t), U = N < MOST ? N : MOST;
     static_assert(N % U == 0, "whole turns");
-#pragma unroll(U == 1 ? 4 : 1)
+#pragma unroll 1
     for (int from = 0; from < N; from += U) {
       out_t o[U];
-      if (onto) {
+      if (onto && vec) {  // (past the end: the last row, the last whole run)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int e = (from + u) * 64 + lane, row = r0 + e / CH, col = first + e % CH * PER;
-          if (vec && row < rows && col + PER <= cols) o[u] = *reinterpret_cast<const out_t*>(c + (int64_t)row * ldc + col);
+          const int e = (from + u) * 64 + lane, row = min(r0 + e / CH, rows - 1), col = min(first + e % CH * PER, cols / PER * PER - PER);
+          o[u] = *reinterpret_cast<const out_t*>(c + (int64_t)row * ldc + col);
         }
       }
 #pragma unroll
