@@ -1,7 +1,9 @@
 /*
  * dla.h - C ABI of the MI355X (gfx950) dense linear-algebra kernels that the
  * paper's autotuner compiles and times: 3mm, LU without pivoting, Cholesky
- * (paper, Section "Linear Algebra Benchmarks").
+ * (paper, Section "Linear Algebra Benchmarks"); the solves and products beside
+ * them; and the products of language models in microscaled 4-bit floating point
+ * (mx4_*).
  *
  * Conventions that hold for every entry point
  *   - Matrices are ROW-MAJOR (the paper's X[i, j] indexing in the 3mm
@@ -392,11 +394,11 @@ int dla_block_size_supported(dla_dtype dt, int nb);
 int dla_default_params(int kernel, int64_t n, dla_dtype dt, void* out);
 
 /*
- * Optional per-phase timing for benchmarks.  While enabled, the factorisations
- * and mm3 bracket every launch of the named phase with events on the stream
+ * Optional per-phase timing for benchmarks.  While enabled, the factorisations,
+ * mm3 and the mx4_ products (these as whole calls) bracket every launch of the named phase with events on the stream
  * the kernel runs on.  dla_profile_read synchronises those events and returns
  * accumulated milliseconds and launch counts, then clears them.
- * Phases: 0 = tiled GEMM (3mm products, strip updates, caller-tiled trailing updates),
+ * Phases: 0 = tiled GEMM (3mm products, strip updates, caller-tiled trailing updates, mx4_gemm, mx4_apply),
  * 1 = diagonal block, 2 = panel solves and head update, 3 = bulk trailing update (default schedule).
  * Profiling is per process, not thread safe, and perturbs the pipeline; leave
  * it off when timing whole calls.

@@ -52,7 +52,8 @@ int launch(const MxGemmArgs& g, const MxPlan& plan, hipStream_t stream) {
     case 48: return launch_direct<3, 3, 3>(g, stream);
     case 64: return launch_direct<4, 2, 2>(g, stream);
   }
-  return g.dt == DLA_F32 ? launch_typed<float>(g, plan, stream) : g.dt == DLA_BF16 ? launch_typed<__bf16>(g, plan, stream) : launch_typed<_Float16>(g, plan, stream);
+  if (g.dt == DLA_F32) return launch_typed<float>(g, plan, stream);
+  return g.dt == DLA_BF16 ? launch_typed<__bf16>(g, plan, stream) : launch_typed<_Float16>(g, plan, stream);
 }
 
 }  // namespace

@@ -522,3 +522,65 @@ def test_search_over_the_schedules(B, capsys, tmp_path, kernel, op, shape, dtype
     assert len(rows) == 9 and out["kernel"] == kernel and out["evaluations"] == 8
     assert 0.0 < out["best_runtime_ms"] <= float(rows[1].split(",")[-2]) + 1e-3
     assert len(out["best"]["tile"]) == 2 and out["best"]["splits"] >= 1
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gemm_onto_aligned_rows_that_end_anywhere(B, dtype):
+    """C in rows of whole 16 bytes, its last columns and rows inside a lane's run, a wave's part, a tile.  All sums are exact."""
+    import torch
+    rng = np.random.default_rng(17)
+    k = 200
+    for m, n in ((1, 1), (2, 3), (33, 5), (64, 8), (70, 9), (130, 131), (257, 63), (100, 260), (300, 193)):
+        ac, as_ = O.random_codes(rng, m, k)
+        bc, bs = O.random_codes(rng, n, k)
+        c0 = rng.integers(-8, 9, (m, n)).astype(float)
+        want = rounded(O.values(ac, as_) @ O.values(bc, bs).T + c0, dtype)
+        a, b = micro(B, ac, as_, k), micro(B, bc, bs, k)
+        for tile in ((128, 128), (256, 256), (16, 32)):
+            announce(f"mx4_gemm onto {dtype} {m} x {n} tile {tile}")
+            full = torch.full((m + 2, (n + 7) // 8 * 8 + 16), float("nan"), dtype=getattr(torch, dtype), device="cuda")
+            c = full[1:m + 1, 8:8 + n]
+            assert c.data_ptr() % 16 == 0 and c.stride(0) % 8 == 0
+            c.copy_(torch.from_numpy(c0).to(c.dtype))
+            B.mx4_gemm(1, a, b, c, B.Mx4Params(*tile, 1))
+            assert np.array_equal(f64(c), want)
+            assert int(torch.isnan(full).sum()) == full.numel() - m * n
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_rows_by_many_columns(B, dtype):
+    """At and above the four rows that have a kernel of their own, with more and fewer workgroups than compute units."""
+    rng = np.random.default_rng(18)
+    for m, n, k in ((2, 8200, 260), (4, 8200, 128), (5, 8200, 130), (4, 100, 1000), (5, 60, 900), (17, 4200, 384)):
+        wc, ws = O.random_codes(rng, n, k)
+        xc, xs = O.random_codes(rng, m, k)
+        w, xv = micro(B, wc, ws, k), O.values(xc, xs)[:, :k]
+        wv = O.values(wc, ws)[:, :k]
+        x = rng.integers(-8, 9, (m, k)).astype(float)
+        for tile in ((16, 32), (0, 0)):
+            announce(f"few rows {dtype} {m} x {n} x {k} tile {tile}")
+            p = B.Mx4Params(*tile, 1 if tile[0] else 0)
+            _, y = put(np.zeros((m, n)), dtype)
+            B.mx4_apply(0, put(x, dtype)[1], w, y, p)
+            assert np.array_equal(f64(y), rounded(x @ wv.T, dtype))
+            B.mx4_gemm(0, micro(B, xc, xs, k), w, y, p)
+            assert np.array_equal(f64(y), rounded(xv @ wv.T, dtype))
+
+
+def test_profile_counts_the_products(B):
+    import torch
+    announce("mx4 profile")
+    w, y = B.mx4_empty(50, 300), torch.empty((9, 50), device="cuda")
+    x = torch.ones((50, 300), device="cuda")
+    B.mx4_quantize(x, w)
+    a = B.mx4_empty(9, 300)
+    B.mx4_quantize(x[:9], a)
+    B.profile_enable(True)
+    try:
+        B.mx4_gemm(0, a, w, y)
+        B.mx4_apply(0, x[:9], w, y)
+    finally:
+        B.profile_enable(False)
+    ms, calls, flops = B.profile_read(B.PHASE_GEMM)
+    assert calls == 2 and ms > 0 and flops == 2 * 2 * 9 * 50 * 300
+    assert (f64(y) == 300).all()

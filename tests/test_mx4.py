@@ -230,3 +230,30 @@ def test_every_tile_is_the_choice_for_some_sizes(B):
                             d = B.mx4_default_params(kernel, op, m, n, k, dt)
                             left.discard((d.tile_m, d.tile_n))
                 assert not left, (kernel, op, dt, left)
+
+
+def test_apply_workspace_follows_how_x_lies(B):
+    """X that a kernel takes as it lies needs no copy; any other needs room for one, which the call insists on."""
+    m, n, k = 64, 512, 256
+    query, f = B.lib.mx4_apply_workspace_bytes, B.lib.mx4_apply
+
+    def need(op, x, ldx, dt, terms_n=n, terms_k=k):
+        return query(op, x, ldx, dt, m, terms_n, terms_k, ctypes.byref(one))
+
+    for op in (0, 1):
+        for tile in ((16, 32), (128, 128)) if op == 0 else ((128, 128),):
+            one = B.Mx4Params(*tile, 1)
+            terms = n if op else k
+            assert need(op, FAKE, terms, B.DLA_BF16) == 0
+            assert need(op, ctypes.c_void_p(0x1002), terms, B.DLA_BF16) >= m * terms * 2
+            assert need(op, FAKE, terms + 1, B.DLA_BF16) >= m * terms * 2
+            assert need(op, FAKE, terms, B.DLA_F32) >= m * terms * 6
+            assert (need(op, FAKE, terms, B.DLA_F16) == 0) == (tile == (16, 32))  # two bf16 terms for the other
+            got = need(op, FAKE, terms + 1, B.DLA_BF16)
+            args = (op, FAKE, terms + 1, B.DLA_BF16, FAKE, k // 2, FAKE, k // 32, FAKE, max(n, k), B.DLA_F32, m, n, k, ctypes.byref(one))
+            assert f(*args, None, got, None) == B.DLA_ERR_WORKSPACE
+            assert f(*args, FAKE, got - 1, None) == B.DLA_ERR_WORKSPACE
+            assert f(*args, ctypes.c_void_p(0x1080), got, None) == B.DLA_ERR_WORKSPACE
+    one = B.Mx4Params(128, 128, 1)
+    assert need(0, FAKE, k - 8, B.DLA_BF16, n, k - 8) >= m * (k - 8) * 2  # no whole steps
+    assert query(2, FAKE, k, B.DLA_BF16, m, n, k, None) == query(0, FAKE, k, B.DLA_F64, m, n, k, None) == query(0, FAKE, k, B.DLA_BF16, 0, n, k, None) == 0
