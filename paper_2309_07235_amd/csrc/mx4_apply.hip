@@ -84,26 +84,28 @@ size_t copy_bytes(const MxPlan& plan, int64_t m, int64_t terms, dla_dtype dt) {
   return ((size_t)(m * count) + 255) / 256 * 256;
 }
 
-template <typename T, int TERMS, int MB, int XI, int WV, int DW>
+template <typename T, int TERMS, int MB, int XI, int WV, int DW, int DX>
 int launch_direct_as(const MxApplyArgs& g, hipStream_t stream) {
-  hipLaunchKernelGGL((mx4_apply_direct_kernel<T, TERMS, MB, XI, WV, DW>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(WV * 64), 0, stream, g);
+  hipLaunchKernelGGL((mx4_apply_direct_kernel<T, TERMS, MB, XI, WV, DW, DX>), dim3((unsigned)(g.tiles_m * g.tiles_n * g.splits)), dim3(WV * 64), 0, stream, g);
   return launch_status(__func__);
 }
 
-// How many waves and how far ahead is what the LDS holds: up to 16 rows of 16 bits (4 of fp32), eight waves where there is one workgroup
-// for each of the 256 units at most, and four, so that several fit a unit, where there are more.
+// How many waves and how far ahead is what the LDS holds.  Up to 16 rows of 16 bits (4 of fp32): eight waves where there is one workgroup
+// for each of the 256 units at most, and four, so that several fit a unit, where there are more.  Above, eight waves with one step of
+// X ahead rather than four with two, so that one wave's products hide what the other of its SIMD waits for: 48 rows of fp16 by
+// 8192 x 8192 17.5 us for 19.8, 64 by 4096 x 4096 10.9 for 13.2 (bf16, which has half the work between its loads, the same in both).
 template <typename T, int TERMS>
 int launch_direct(const MxApplyArgs& g, int tile_m, hipStream_t stream) {
   const bool many = (int64_t)g.tiles_m * g.tiles_n * g.splits > 256;
-  if (tile_m == 16 && g.m <= 4) return many ? launch_direct_as<T, TERMS, 1, 1, 4, 4>(g, stream) : launch_direct_as<T, TERMS, 1, 1, 8, 4>(g, stream);
+  if (tile_m == 16 && g.m <= 4) return many ? launch_direct_as<T, TERMS, 1, 1, 4, 4, 2>(g, stream) : launch_direct_as<T, TERMS, 1, 1, 8, 4, 2>(g, stream);
   if constexpr (TERMS == 3) {
-    return launch_direct_as<T, TERMS, 1, 4, 4, 4>(g, stream);
+    return launch_direct_as<T, TERMS, 1, 4, 4, 4, 2>(g, stream);
   } else {
     switch (tile_m) {
-      case 16: return many ? launch_direct_as<T, 1, 1, 4, 4, 4>(g, stream) : launch_direct_as<T, 1, 1, 4, 8, 4>(g, stream);
-      case 32: return launch_direct_as<T, 1, 2, 8, 4, 6>(g, stream);
-      case 48: return launch_direct_as<T, 1, 3, 12, 4, 6>(g, stream);
-      default: return launch_direct_as<T, 1, 4, 16, 4, 3>(g, stream);
+      case 16: return many ? launch_direct_as<T, 1, 1, 4, 4, 4, 2>(g, stream) : launch_direct_as<T, 1, 1, 4, 8, 4, 2>(g, stream);
+      case 32: return launch_direct_as<T, 1, 2, 8, 8, 4, 1>(g, stream);
+      case 48: return launch_direct_as<T, 1, 3, 12, 8, 3, 1>(g, stream);
+      default: return launch_direct_as<T, 1, 4, 16, 8, 1, 1>(g, stream);
     }
   }
 }

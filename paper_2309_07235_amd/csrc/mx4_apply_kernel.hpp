@@ -39,7 +39,7 @@ __device__ __forceinline__ void mx_terms_of(T __attribute__((ext_vector_type(8))
 }
 
 // Few rows of X: what bounds the call is reading W once.  The WV waves of a workgroup share the sum over k, each with a run of
-// steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X two.  Through LDS, because the matrix instructions
+// steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X DX.  Through LDS, because the matrix instructions
 // want neighbouring lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16 (16384 x 4096 weights,
 // one row, bf16: 9.2 us, 3.9 TB/s; 16 us with loads to registers).  With 48 rows of fp16 by 8192 x 8192, 21 us, it is the products and
 // the scaling of their sums.
@@ -50,12 +50,12 @@ __device__ __forceinline__ void mx_terms_of(T __attribute__((ext_vector_type(8))
 //                they would leave the type's range); the sum is scaled on its way to the running one, in fp32.
 // XI: loads of X a plane and step, of four rows each: one where there are at most four rows, whose place the others of the instruction read
 // too (they reach rows of the result that are not stored).
-template <typename T, int TERMS, int MB, int XI, int WV, int DW>
+template <typename T, int TERMS, int MB, int XI, int WV, int DW, int DX>
 __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g) {
   constexpr int NB = 2, TM = MB * 16, TN = NB * 16, XR = XI * 4;
   constexpr bool F16 = std::is_same<T, _Float16>::value;
   static_assert(sizeof(T) == 2 && (XR == TM || XR == 4) && (!F16 || TERMS == 1), "rows of 256 bytes a step, all of them or four");
-  constexpr int W_RING = DW * NB * 64, X_STAGE = TERMS * XR * 16, RING = W_RING + 2 * X_STAGE + 2 * TN;  // units of 16 bytes
+  constexpr int W_RING = DW * NB * 64, X_STAGE = TERMS * XR * 16, RING = W_RING + DX * X_STAGE + 2 * TN;  // units of 16 bytes
   static_assert(WV * RING * 16 <= 160 * 1024 && RING * 16 >= TM * TN * 4, "LDS");
   typedef T run_t __attribute__((ext_vector_type(8)));
   __shared__ u32x4_t lds[WV * RING];
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
   const int share = split * WV + wave, shares = g.splits * WV;
   const int begin = (int)((int64_t)g.steps * share / shares), end = (int)((int64_t)g.steps * (share + 1) / shares);
   u32x4_t* const ring = lds + wave * RING;
-  const unsigned int at_w = lds_offset(ring), at_x = at_w + W_RING * 16, at_s = at_x + 2 * X_STAGE * 16;
+  const unsigned int at_w = lds_offset(ring), at_x = at_w + W_RING * 16, at_s = at_x + DX * X_STAGE * 16;
 
   // W: a load fills 16 rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4; X: 4 rows of 256 bytes, chunk c of row r at c ^ r % 16
   const uint8_t* const wq = g.w.q + (int64_t)n0 * g.w.ldq;
@@ -116,20 +116,21 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
 #pragma unroll
       for (int i = 0; i < 3; ++i)
         if (begin + i < end) w[i] = *reinterpret_cast<const unsigned int*>(ws + soff + (begin + i) * 4);
-      ring[W_RING + 2 * X_STAGE + lane] = w;
+      ring[W_RING + DX * X_STAGE + lane] = w;
     }
+    // (a step's loads are X's DX steps ahead, then W's DW ahead: here those of the steps before `begin`)
 #pragma unroll
     for (int i = 0; i < DW; ++i) {
+      if (i >= DW - DX) load_x(begin + i - (DW - DX), i - (DW - DX));
       load_w(begin + i, i);
-      if (i >= DW - 2) load_x(begin + i - (DW - 2), i - (DW - 2));
     }
     int slot = 0;
     for (int s = begin; s < end; ++s) {
       const int i = s - begin, chunk = i >> 2;
-      wait_loads<NB + TERMS * XI>();  // this step has arrived: only the next one's loads of X, and W's beside them, are younger
+      wait_loads<(DX - 1) * TERMS * XI + (DW > DX ? DX : DX - 1) * NB>();  // this step's X and W have arrived
       const u32x4_t* const wr = ring + slot * NB * 64;
-      const u32x4_t* const xr = ring + W_RING + (i & 1) * X_STAGE;
-      const unsigned int* const sr = reinterpret_cast<const unsigned int*>(ring + W_RING + 2 * X_STAGE + (chunk & 1) * TN) + (g.steps >= 4 ? s - scales_from(chunk) : i);
+      const u32x4_t* const xr = ring + W_RING + i % DX * X_STAGE;
+      const unsigned int* const sr = reinterpret_cast<const unsigned int*>(ring + W_RING + DX * X_STAGE + (chunk & 1) * TN) + (g.steps >= 4 ? s - scales_from(chunk) : i);
       unsigned int w[NB][4], sc[NB];
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
@@ -150,8 +151,8 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
           }
       wait_lds();  // (before what was read is overwritten)
       if ((i & 3) == 0 && s + 4 < end) load_s(chunk + 1);
+      load_x(s + DX, i % DX);
       load_w(s + DW, slot);
-      load_x(s + 2, i & 1);
       slot = slot + 1 == DW ? 0 : slot + 1;
 
       float own[NB];
