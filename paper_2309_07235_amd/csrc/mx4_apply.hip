@@ -8,26 +8,26 @@ namespace {
 constexpr int kDirect = 32;  // columns of a direct kernel's tile
 
 // The tiles.  The direct kernels are for op 0; more than 16 rows of fp32 there, and two or three terms of 256 rows, do not fit the LDS.  The
-// costs are fitted to 4000 timings of 190 products (1 to 4096 rows, 128 to 8192 columns and terms, every tile, 1 to 32 splits): the choice takes
+// costs are fitted to 8000 timings of 390 products (1 to 4096 rows, 128 to 8192 columns and terms, every tile, 1 to 32 splits): the choice takes
 // 1 to 6 % longer in the mean than the best of them, by operation and type.
 const MxTileCost kForwardBf16[] = {
-    {16, 32, 7.02f, 2.86f, 0.0348f, 0.0982f, 0.702f},
-    {32, 32, 7.92f, 1.94f, 0.0926f, 0.175f, 0.954f},
-    {48, 32, 7.65f, 2.03f, 0.141f, 0.256f, 0.994f},
-    {64, 32, 8.19f, 1.08f, 0.266f, 0.279f, 1.0f},
-    {32, 128, 7.67f, 0.495f, 0.502f, 0.358f, 1.42f},
-    {64, 128, 6.43f, 1.55f, 0.661f, 0.455f, 2.78f},
-    {128, 128, 6.81f, 1.36f, 1.02f, 0.782f, 2.59f},
-    {256, 256, 9.62f, 2.93f, 0.574f, 2.53f, 0.998f},
+    {16, 32, 4.94f, 4.38f, 0.0397f, 0.0881f, 0.916f},
+    {32, 32, 3.46f, 5.91f, 0.0355f, 0.15f, 2.25f},
+    {48, 32, 2.43f, 6.68f, 0.0651f, 0.186f, 2.79f},
+    {64, 32, 0.967f, 8.39f, 0.0789f, 0.213f, 3.52f},
+    {32, 128, 6.73f, 1.25f, 0.464f, 0.345f, 0.912f},
+    {64, 128, 6.98f, 2.09f, 0.28f, 0.54f, 0.877f},
+    {128, 128, 6.9f, 1.34f, 0.929f, 0.74f, 1.26f},
+    {256, 256, 9.24f, 2.73f, 0.432f, 2.34f, 1.04f},
 };
 const MxTileCost kForwardF16[] = {
-    {16, 32, 6.86f, 3.31f, 0.0586f, 0.0792f, 0.924f},
-    {32, 32, 9.58f, 0.984f, 0.106f, 0.106f, 0.984f},
-    {48, 32, 9.34f, 1.01f, 0.162f, 0.162f, 1.01f},
-    {64, 32, 6.08f, 3.98f, 0.17f, 0.207f, 3.07f},
-    {32, 128, 9.12f, 1.48f, 0.352f, 0.576f, 1.01f},
-    {64, 128, 9.27f, 1.9f, 0.345f, 0.815f, 0.967f},
-    {128, 128, 2.83f, 8.18f, 1.61f, 0.5f, 0.994f},
+    {16, 32, 5.2f, 3.94f, 0.0511f, 0.106f, 0.749f},
+    {32, 32, 1.93f, 7.79f, 0.0108f, 0.18f, 2.39f},
+    {48, 32, 1.55f, 7.34f, 0.0771f, 0.209f, 3.11f},
+    {64, 32, 7.06f, 1.72f, 0.167f, 0.256f, 1.0f},
+    {32, 128, 8.07f, 1.59f, 0.583f, 0.504f, 1.16f},
+    {64, 128, 7.98f, 2.99f, 0.385f, 0.834f, 1.0f},
+    {128, 128, 9.22f, 2.26f, 0.48f, 1.74f, 1.0f},
 };
 const MxTileCost kForwardF32[] = {
     {16, 32, 3.15f, 8.18f, 0.0402f, 0.198f, 2.19f},
