@@ -41,8 +41,8 @@ __device__ __forceinline__ void mx_terms_of(T __attribute__((ext_vector_type(8))
 // Few rows of X: what bounds the call is reading W once.  The WV waves of a workgroup share the sum over k, each with a run of
 // steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X DX.  Through LDS, because the matrix instructions
 // want neighbouring lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16 (16384 x 4096 weights,
-// one row, bf16: 9.2 us, 3.9 TB/s; 16 us with loads to registers).  With 48 rows of fp16 by 8192 x 8192, 21 us, it is the products and
-// the scaling of their sums.
+// one row, bf16: 9.2 us, 3.9 TB/s; 16 us with loads to registers).  With 48 rows of fp16 by 8192 x 8192, 17.5 us, it is X too, which each of
+// 256 workgroups reads, and the scaling of the products' sums.
 //   bf16, fp32   a lane's block of W is made bf16 with its scale; X is one plane of bf16 or, for fp32, three that add up to it (made by a
 //                launch in front: made here, by every workgroup, they cost more than the rest of the call); instruction b takes
 //                eight elements of every lane's block;

@@ -584,3 +584,16 @@ def test_profile_counts_the_products(B):
     ms, calls, flops = B.profile_read(B.PHASE_GEMM)
     assert calls == 2 and ms > 0 and flops == 2 * 2 * 9 * 50 * 300
     assert (f64(y) == 300).all()
+
+
+def test_quantize_rows_of_many_tiles(B):
+    """64 tiles of columns and more a row, of which groups go to one cache; the last group is not whole."""
+    rng = np.random.default_rng(19)
+    for rows, cols in ((1, 8192), (130, 8065), (129, 8200), (300, 10000)):
+        announce(f"quantize wide {rows} x {cols}")
+        x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-6, 7, (rows, cols)))
+        _, xd = put(x, "bfloat16")
+        q, qt = room(B, rows, cols, 1), room(B, cols, rows, 1)
+        B.mx4_quantize(xd, q, qt)
+        check_form(q, f64(xd), 1)
+        check_form(qt, f64(xd).T, 1)
