@@ -597,3 +597,51 @@ def test_quantize_rows_of_many_tiles(B):
         B.mx4_quantize(xd, q, qt)
         check_form(q, f64(xd), 1)
         check_form(qt, f64(xd).T, 1)
+
+
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_apply_subnormal_x(B, dtype, op):
+    """The type's smallest values count: multiples of its smallest step (fp32: of 2^-133, the least that the terms hold), products
+    and sums of which fp32 holds exactly with weights of 2^2 and more."""
+    import torch
+    rng = np.random.default_rng(20)
+    step = {"float32": 2.0 ** -133, "bfloat16": 2.0 ** -133, "float16": 2.0 ** -24}[dtype]
+    m, n, k = 33, 70, 200
+    wc, ws = O.random_codes(rng, n, k, 131, 133)
+    wv = O.values(wc, ws)[:, :k]
+    x = rng.integers(-100, 101, (m, n if op else k)) * step
+    _, xd = put(x, dtype)
+    assert np.array_equal(f64(xd), x)
+    want = x @ (wv if op else wv.T)
+    w = micro(B, wc, ws, k)
+    for rows in (m, 3):
+        for p in apply_params(B, op, dtype):
+            if not legal_apply(B, op, p, x.shape[1]):
+                continue
+            announce(f"mx4_apply subnormal {dtype} op {op} {rows} rows {p}")
+            y = torch.empty((rows, want.shape[1]), device="cuda")
+            B.mx4_apply(op, xd[:rows], w, y, p)
+            assert np.array_equal(f64(y), want[:rows]), p
+
+
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_apply_smallest_weights(B, dtype, op):
+    """Weights at and next to the least scale, 2^-127, some of them subnormal in bf16; all sums are exact in fp32."""
+    import torch
+    rng = np.random.default_rng(21)
+    m, n, k = 20, 70, 200
+    wc, ws = O.random_codes(rng, n, k, 0, 3)
+    wv = O.values(wc, ws)[:, :k]
+    x = rng.integers(-8, 9, (m, n if op else k)).astype(float)
+    want = x @ (wv if op else wv.T)
+    w = micro(B, wc, ws, k)
+    for rows in (m, 3):
+        for p in apply_params(B, op, dtype):
+            if not legal_apply(B, op, p, x.shape[1]):
+                continue
+            announce(f"mx4_apply smallest weights {dtype} op {op} {rows} rows {p}")
+            y = torch.empty((rows, want.shape[1]), device="cuda")
+            B.mx4_apply(op, put(x[:rows], dtype)[1], w, y, p)
+            assert np.array_equal(f64(y), want[:rows]), p
