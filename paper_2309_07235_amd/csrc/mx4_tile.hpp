@@ -96,7 +96,7 @@ __device__ __forceinline__ void mx_store_tile(u32x4_t* lds, const f32x16_t (&acc
 #pragma unroll 1
     for (int from = 0; from < N; from += U) {
       out_t o[U];
-      if (onto && vec) {  // (past the end: the last row, the last whole run)
+      if (onto && vec) {  // (past the end the last row or whole run, which is not used there and may just be written)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int e = (from + u) * 64 + lane, row = min(r0 + e / CH, rows - 1), col = min(first + e % CH * PER, cols / PER * PER - PER);
