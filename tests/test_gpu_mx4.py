@@ -645,3 +645,35 @@ def test_apply_smallest_weights(B, dtype, op):
             y = torch.empty((rows, want.shape[1]), device="cuda")
             B.mx4_apply(op, put(x[:rows], dtype)[1], w, y, p)
             assert np.array_equal(f64(y), want[:rows]), p
+
+
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_apply_keeps_every_bit_of_x(B, dtype, op):
+    """A row of X holds one value, an odd integer of all the type's bits, at a term of its own; weights are powers of two.  Each result is
+    one product, exact in fp32: a term of X that is lost, or read from another place, changes its last bits."""
+    import torch
+    rng = np.random.default_rng(22)
+    bits = {"float32": 24, "bfloat16": 8, "float16": 11}[dtype]
+    most, out, terms = 130, 70, 390
+    n, k = (terms, out) if op else (out, terms)
+    wc, ws = O.random_codes(rng, n, k, 118, 131)
+    wc[:, :k] = rng.choice(np.array([1, 2, 4, 6, 9, 10, 12, 14], np.uint8), (n, k))
+    assert (np.log2(np.abs(O.VALUES[[1, 2, 4, 6]])) == [-1, 0, 1, 2]).all()
+    wv = O.values(wc, ws)[:, :k]
+    at = (np.arange(most) * 3 + rng.integers(0, 3, most)) % terms
+    at[[0, 1, 2]] = terms - 1, 0, terms - 2
+    x = np.zeros((most, terms))
+    x[np.arange(most), at] = (2 ** (bits - 1) + 2 * rng.integers(0, 2 ** (bits - 2), most) + 1) * np.where(rng.integers(0, 2, most), 1.0, -1.0) * 2.0 ** -bits
+    want = x @ (wv if op else wv.T)
+    w = micro(B, wc, ws, k)
+    for rows, pad in ((3, 0), (16, 1), (33, 8), (most, 0)):
+        _, xd = put(x[:rows], dtype, pad)
+        assert np.array_equal(f64(xd), x[:rows])
+        for p in apply_params(B, op, dtype):
+            if not legal_apply(B, op, p, terms):
+                continue
+            announce(f"mx4_apply every bit {dtype} op {op} {rows} rows {p}")
+            y = torch.empty((rows, out), device="cuda")
+            B.mx4_apply(op, xd, w, y, p)
+            assert np.array_equal(f64(y), want[:rows]), p
