@@ -357,6 +357,8 @@ size_t mx4_gemm_workspace_bytes(int64_t m, int64_t n, int64_t k, const mx4_param
  * X in dt and Y in dt_y, each DLA_F32, DLA_BF16 or DLA_F16.  Nothing of X or W is rounded: X goes into the bf16 matrix
  * instructions as one (DLA_BF16), two (DLA_F16) or three (DLA_F32) bf16 terms that add up to it (DLA_F32: down to 2^-133), few
  * rows of DLA_F16 into the fp16 ones as they are; sums are fp32, Y is rounded once.  The sum has at most 2^21 terms (else DLA_ERR_TOO_LARGE).
+ * Weights of 2^128 and more (scales of 2^126 and 2^127, which mx4_quantize does not write) count as they are too, but the parts of Y
+ * that they go into take some hundred times as long.
  *   d_workspace / workspace_bytes   as for mx4_gemm.  The query takes X's address and leading dimension (X is not read): a kernel that
  *                                   cannot take X as it lies (rows not aligned to 16 bytes, a sum that is not a whole number of
  *                                   steps, terms of DLA_F32 or DLA_F16) reads a copy that a first launch leaves in the workspace.

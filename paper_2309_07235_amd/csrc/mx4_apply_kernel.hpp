@@ -38,6 +38,113 @@ __device__ __forceinline__ void mx_terms_of(T __attribute__((ext_vector_type(8))
   }
 }
 
+// Scales of 2^126 and 2^127 (no weight that mx4_quantize writes has them) take elements from 4 and from 2 on out of bf16's range: they go
+// into the products as infinities, and all sums of their column become infinities or, where a term of X is zero, NaN.  So a wave
+// with a finite sum in each column has met none.  Any other looks for such scales, and if it finds one computes its
+// values again, each by itself from memory, in fp32 and with weights 2^-4 as large as they are.  (Looking for them in the main loop made
+// gradients 2 to 5 % slower; 1024 rows by 4096 x 4096 with a scale of 2^127 in each tile take 9 ms, the gradient 33.)
+
+// Whether no sum of some column is finite.  A lane's registers are N times 16 columns (of M blocks of 32 rows, ACROSS, 32 lanes), or rows of N columns
+// (of M blocks of 16, every sixteenth lane).
+template <bool ACROSS, typename V, int M, int N>
+__device__ __forceinline__ bool mx_column_lost(const V (&acc)[M][N]) {
+  constexpr int R = (int)(sizeof(V) / 4);
+  float any = 0.0f;  // (a product with zero is zero or a NaN)
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int v = 0; v < R; ++v) any = __builtin_fmaf(acc[i][j][v], 0.0f, any);
+  if (__builtin_expect(!__any(any != 0.0f), 1)) return false;
+  bool lost = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    unsigned long long all = ~0ull;
+#pragma unroll
+    for (int v = 0; v < R; ++v) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) all &= __ballot(acc[i][j][v] * 0.0f != 0.0f);
+      if (ACROSS) {
+        lost |= (unsigned int)all == ~0u || (unsigned int)(all >> 32) == ~0u;
+        all = ~0ull;
+      }
+    }
+    if (!ACROSS) lost |= (all & all >> 16 & all >> 32 & all >> 48 & 0xffffu) != 0;
+  }
+  return lost;
+}
+
+// Whether one of the scales of rows r0 .. r1 - 1 of W, blocks b0 .. b1 - 1, is such a one; b0 is a multiple of four, and so is the end
+// of a row with its padding, whose scales are zero.
+__device__ __forceinline__ bool mx_beyond_along(const Mx4View& w, int lane, int r0, int r1, int b0, int b1) {
+  bool found = false;
+  for (int b = b0 + lane * 4; b < b1; b += 256)
+#pragma unroll 4
+    for (int r = r0; r < min(r1, w.rows); ++r) {
+      const unsigned int four = *reinterpret_cast<const unsigned int*>(w.s + (int64_t)r * w.lds + b);
+      for (int i = 0; i < 32; i += 8) found |= (four >> i & 255u) - 253u < 2u;
+    }
+  return __any(found);
+}
+
+// The same of many rows and the one or two blocks of C columns from c0 (a multiple of C; past w_cols, W's columns with their padding, the last).
+template <int C>
+__device__ __forceinline__ bool mx_beyond_down(const Mx4View& w, int lane, int r0, int r1, int c0, int w_cols) {
+  static_assert(C == 32 || C == 64, "one load a row");
+  typedef typename std::conditional<C == 64, uint16_t, uint8_t>::type load_t;
+  const uint8_t* s = w.s + min(c0, w_cols - C) / 32 + (int64_t)(r0 + lane) * w.lds;
+  bool found = false;
+#pragma unroll 4
+  for (int r = r0 + lane; r < r1; r += 64, s += 64 * w.lds) {
+    const unsigned int v = *reinterpret_cast<const load_t*>(s);
+    found |= (v & 255u) - 253u < 2u;
+    if (C == 64) found |= (v >> 8) - 253u < 2u;
+  }
+  return __any(found);
+}
+
+// Row x times row `row` of W, blocks b0 .. b1 - 1.
+template <int TERMS>
+__device__ __forceinline__ float mx_again_along(const __bf16* x, int64_t plane, const Mx4View& w, int row, int b0, int b1) {
+  typedef __bf16 run_t __attribute__((ext_vector_type(8)));
+  const unsigned int* const q = reinterpret_cast<const unsigned int*>(w.q + (int64_t)row * w.ldq);
+  const uint8_t* const s = w.s + (int64_t)row * w.lds;
+  float sum = 0.0f;
+#pragma unroll 1
+  for (int j = b0 * 4; j < b1 * 4; ++j) {
+    const float f = mx_scale_value(s[j / 4]) * 0.0625f;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) {
+      const run_t r = *reinterpret_cast<const run_t*>(x + t * plane + (int64_t)j * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += (float)r[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(v[i], __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[j] >> (4 * i), 1.0f, 0)[0] * f, sum);
+  }
+  return sum * 16.0f;
+}
+
+// Row x times column `col` of W, rows r0 .. r1 - 1.
+template <int TERMS>
+__device__ __forceinline__ float mx_again_down(const __bf16* x, int64_t plane, const Mx4View& w, int col, int r0, int r1) {
+  float sum = 0.0f;
+#pragma unroll 1
+  for (int r = r0; r < r1; ++r) {
+    float v = 0.0f;
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) v += (float)x[t * plane + r];
+    const unsigned int e = w.q[(int64_t)r * w.ldq + col / 2] >> (col & 1) * 4;
+    const float f = mx_scale_value(w.s[(int64_t)r * w.lds + col / 32]) * 0.0625f;
+    sum = __builtin_fmaf(v, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(e, 1.0f, 0)[0] * f, sum);
+  }
+  return sum * 16.0f;
+}
+
 // Few rows of X: what bounds the call is reading W once.  The WV waves of a workgroup share the sum over k, each with a run of
 // steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X DX.  Through LDS, because the matrix instructions
 // want neighbouring lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16 (16384 x 4096 weights,
@@ -193,12 +300,23 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
   }
   wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
   float* const part = reinterpret_cast<float*>(lds);
+  bool again = false;
+  if constexpr (!F16) again = mx_column_lost<false>(acc) && mx_beyond_along(g.w, lane, n0, n0 + TN, begin * 4, end * 4);
+  if (again) {
+    if constexpr (!F16) {
+#pragma unroll 1
+      for (int e = lane; e < TM * TN; e += 64)
+        part[wave * TM * TN + e] = mx_again_along<TERMS>(static_cast<const T*>(g.x) + (int64_t)min(m0 + e / TN, g.m - 1) * g.ldx, g.plane, g.w,
+                                                         min(n0 + e % TN, g.w.rows - 1), begin * 4, end * 4);
+    }
+  } else {
 #pragma unroll
-  for (int i = 0; i < MB; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) part[wave * TM * TN + (i * 16 + l4 * 4 + v) * TN + j * 16 + l15] = acc[i][j][v];
+        for (int v = 0; v < 4; ++v) part[wave * TM * TN + (i * 16 + l4 * 4 + v) * TN + j * 16 + l15] = acc[i][j][v];
+  }
   __syncthreads();
   for (int e = threadIdx.x; e < TM * TN; e += WV * 64) {
     const int r = m0 + e / TN, c = n0 + e % TN;
@@ -260,6 +378,21 @@ struct MxApplyTileArgs {
   int m, out, w_cols;   // rows and columns of Y; W's columns with their padding
   int steps, splits, tiles_m, tiles_n;  // steps of 64 terms
 };
+
+// A wave's part of the result, R x C from row r0 and column c0, its values those of value(row, col).
+template <int R, int C, typename TY, typename F>
+__device__ __forceinline__ void mx_store_again(const MxApplyTileArgs& g, int split, int lane, int r0, int c0, F value) {
+#pragma unroll 1
+  for (int e = lane; e < R * C; e += 64) {
+    const int row = r0 + e / C, col = c0 + e % C;
+    if (row >= g.m || col >= g.out) continue;
+    const float v = value(row, col);
+    if (g.splits > 1)
+      g.parts[((int64_t)split * g.m + row) * g.out + col] = v;
+    else
+      store_value_as<TY>(g.y, (int64_t)row * g.ldy + col, v, false);
+  }
+}
 
 // How many steps of a tile of Y = X*W^T the LDS holds: up to six where two workgroups of a unit can have them, else as many as one can.
 constexpr int apply_depth(int tm, int tn, int terms) {
@@ -410,6 +543,12 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
     w = next;
   }
   wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
+  if (mx_column_lost<true>(acc) && mx_beyond_along(g.w, lane, n0 + wn0, n0 + wn0 + TN / WN, first * 2, (first + steps) * 2)) {
+    mx_store_again<TM / WM, TN / WN, TY>(g, split, lane, m0 + wm0, n0 + wn0, [&](int row, int col) {
+      return mx_again_along<TERMS>(g.x + row * g.ldx, g.plane, g.w, col, first * 2, (first + steps) * 2);
+    });
+    return;
+  }
   u32x4_t* const room = lds + wave * kMxRoom<TM / WM, TN / WN>;
   if (g.splits > 1)
     mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.m * g.out, g.out, m0 + wm0, n0 + wn0, g.m, g.out, false);
@@ -595,6 +734,12 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
     multiply(odd);
   }
   wait_loads_and_barrier<0>();  // (nothing may arrive in LDS after this)
+  const int last = min((first + steps) * 64, g.w.rows);
+  if (mx_column_lost<true>(acc) && mx_beyond_down<TN / WN>(g.w, lane, first * 64, last, n0 + wn0, g.w_cols)) {
+    mx_store_again<TM / WM, TN / WN, TY>(g, split, lane, m0 + wm0, n0 + wn0,
+                                         [&](int row, int col) { return mx_again_down<TERMS>(g.x + row * g.ldx, g.plane, g.w, col, first * 64, last); });
+    return;
+  }
   u32x4_t* const room = lds + wave * kMxRoom<TM / WM, TN / WN>;
   if (g.splits > 1)
     mx_store_tile<TM / WM, TN / WN, float>(room, acc, lane, g.parts + (int64_t)split * g.m * g.out, g.out, m0 + wm0, n0 + wn0, g.m, g.out, false);

@@ -677,3 +677,38 @@ def test_apply_keeps_every_bit_of_x(B, dtype, op):
             y = torch.empty((rows, out), device="cuda")
             B.mx4_apply(op, xd, w, y, p)
             assert np.array_equal(f64(y), want[:rows]), p
+
+
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_apply_largest_weights(B, dtype, op):
+    """Weights up to 6 * 2^127, past fp32's own range, in blocks of some rows beside ordinary and NaN ones: where X brings the results back
+    into the range they are what they are, exactly (sums of multiples of 2^104 below 2^119, of 2^-23 below 2^-9 beside them), whichever
+    tile computes them, and zeros of X stay zeros."""
+    import torch
+    rng = np.random.default_rng(23)
+    m, n, k = 300, 290, 300
+    wc, ws = O.random_codes(rng, n, k, 125, 127)
+    big = rng.choice(n, 40, replace=False)
+    ws[big, :-(-k // 32)] = rng.integers(252, 255, (40, -(-k // 32)))
+    ws[big[3], 4] = 255
+    wv = O.values(wc, ws)[:, :k]
+    x = rng.integers(-8, 9, (m, n if op else k)) * 2.0 ** -20
+    x[7] = 0.0
+    if op:  # a row of Y is made of rows of W that are all large or all ordinary
+        x[::2, big] = 0.0
+        x[1::2, np.setdiff1d(np.arange(n), big)] = 0.0
+    want = x @ (wv if op else wv.T)
+    w = micro(B, wc, ws, k)
+    for rows in (m, 40, 3):
+        _, xd = put(x[:rows], dtype, rows % 2)
+        assert np.array_equal(f64(xd), x[:rows])
+        for i, p in enumerate(apply_params(B, op, dtype)):
+            if not legal_apply(B, op, p, x.shape[1]):
+                continue
+            for dtype_y in ("float32", TYPES[1 + i % 2]):
+                announce(f"mx4_apply largest weights {dtype} to {dtype_y} op {op} {rows} rows {p}")
+                full, y = put(np.zeros((rows, want.shape[1])), dtype_y, i % 3)
+                B.mx4_apply(op, xd, w, y, p)
+                assert np.array_equal(f64(y), rounded(want[:rows], dtype_y), equal_nan=True), p
+                assert int(torch.isnan(full).sum()) == full.numel() - y.numel() + int(np.isnan(want[:rows]).sum())
