@@ -125,9 +125,8 @@ int launch_planes(const void* x, int64_t ldx, int64_t m, int64_t terms, int64_t 
   const int64_t per_row = to_ld / 8;
   const unsigned int groups = mx4_grid_for(m * per_row, 256);
   if (!groups) return DLA_ERR_TOO_LARGE;
-  const bool vec = (uintptr_t)x % 16 == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
   hipLaunchKernelGGL((mx4_planes_kernel<T, MxType<DT>::kTerms>), dim3(groups), dim3(256), 0, stream, static_cast<const T*>(x), ldx, m, terms,
-                     (int)per_row, vec, static_cast<bf16x8_t*>(planes));
+                     (int)per_row, static_cast<bf16x8_t*>(planes));
   return launch_status(__func__);
 }
 

@@ -348,17 +348,18 @@ __global__ void __launch_bounds__(256) mx4_copy_kernel(const T* x, int64_t ldx, 
 // X as TERMS planes of bf16 that add up to it, rows of `wide` (a multiple of 64) with zeros behind `cols`: what the tile kernel
 // multiplies where X itself is not bf16 in whole, aligned rows.
 template <typename T, int TERMS>
-__global__ void __launch_bounds__(256) mx4_planes_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int per_row, bool vec, bf16x8_t* planes) {
+__global__ void __launch_bounds__(256) mx4_planes_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int per_row, bf16x8_t* planes) {
   const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
   const unsigned int at = (unsigned int)(first - row0 * per_row) + threadIdx.x;
   const int64_t row = row0 + at / (unsigned int)per_row, chunk = at % (unsigned int)per_row;
   if (row >= rows) return;
   typedef T run_t __attribute__((ext_vector_type(8)));
+  typedef T load_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));  // (one access of eight needs no more alignment than one element)
   const T* const p = x + row * ldx + chunk * 8;
   const int64_t left = cols - chunk * 8;
   run_t r;
-  if (vec && left >= 8) {
-    r = *reinterpret_cast<const run_t*>(p);
+  if (left >= 8) {
+    r = *reinterpret_cast<const load_t*>(p);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = i < left ? p[i] : (T)0.0f;

@@ -712,3 +712,32 @@ def test_apply_largest_weights(B, dtype, op):
                 B.mx4_apply(op, xd, w, y, p)
                 assert np.array_equal(f64(y), rounded(want[:rows], dtype_y), equal_nan=True), p
                 assert int(torch.isnan(full).sum()) == full.numel() - y.numel() + int(np.isnan(want[:rows]).sum())
+
+
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_apply_rows_at_every_alignment(B, dtype, op):
+    """X at each place inside 32 bytes, its rows apart by each remainder of 32 bytes: what a row's first access may be aligned to.
+    Integers up to 8 and scales 2^-1 and 1, so every sum is exact."""
+    import torch
+    rng = np.random.default_rng(24)
+    m, n, k = 5, 96, 104
+    wc, ws = O.random_codes(rng, n, k)
+    wv = O.values(wc, ws)[:, :k]
+    w = micro(B, wc, ws, k)
+    terms, out = (n, k) if op else (k, n)
+    dt = getattr(torch, dtype)
+    per = 32 // dt.itemsize
+    x = rng.integers(-8, 9, (m, terms)).astype(float)
+    want = rounded(x @ (wv if op else wv.T), dtype)
+    for first in range(per):
+        for more in range(per):
+            ldx = terms + per + more
+            full = torch.full((m * ldx + first,), float("nan"), dtype=dt, device="cuda")
+            xd = full[first:].view(m, ldx)[:, :terms]
+            xd.copy_(torch.from_numpy(x).to(dt))
+            assert xd.data_ptr() % 32 == first * dt.itemsize and xd.stride(0) == ldx
+            y = torch.empty((m, out), dtype=dt, device="cuda")
+            announce(f"mx4_apply alignment {dtype} op {op} first {first} ldx {ldx}")
+            B.mx4_apply(op, xd, w, y)
+            assert np.array_equal(f64(y), want), (first, ldx)
