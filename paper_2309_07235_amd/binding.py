@@ -432,7 +432,7 @@ def _leading(t, name: str) -> int:
 
 def mx4_padded(cols: int) -> int:
     """The columns that a row of a microscaled matrix holds, padding included (see dla.h: mx4_padded)."""
-    return -(-cols // 128) * 128
+    return lib.mx4_padded(cols)
 
 
 def mx4_empty(rows: int, cols: int, device="cuda") -> Mx4:

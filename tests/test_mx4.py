@@ -257,3 +257,9 @@ def test_apply_workspace_follows_how_x_lies(B):
     one = B.Mx4Params(128, 128, 1)
     assert need(0, FAKE, k - 8, B.DLA_BF16, n, k - 8) >= m * (k - 8) * 2  # no whole steps
     assert query(2, FAKE, k, B.DLA_BF16, m, n, k, None) == query(0, FAKE, k, B.DLA_F64, m, n, k, None) == query(0, FAKE, k, B.DLA_BF16, 0, n, k, None) == 0
+
+
+def test_padded_columns_are_the_librarys(B):
+    for cols in (-1000, -200, -128, -1, 0, 1, 127, 128, 129, 1801, 1 << 30, (1 << 30) + 1):
+        assert B.mx4_padded(cols) == B.lib.mx4_padded(cols), cols
+    assert B.mx4_padded(-200) == 0 and B.mx4_padded(129) == 256
