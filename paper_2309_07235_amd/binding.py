@@ -414,7 +414,7 @@ class Mx4:
         if s.get_device() != device:
             raise ValueError("Mx4: q and s on different devices")
         self.q, self.s, self.rows, self.cols, self._device = q, s, rows, cols, device
-        self._ldq, self._lds = (row_q, row_s) if rows > 1 else (per_q, per_s)
+        self._ldq, self._lds = (row_q, row_s) if rows > 1 else (wide // 2, wide // 32)  # (one row has no distance to the next)
 
     def _args(self):
         return self.q.data_ptr() or None, self._ldq, self.s.data_ptr() or None, self._lds

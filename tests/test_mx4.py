@@ -263,3 +263,15 @@ def test_padded_columns_are_the_librarys(B):
     for cols in (-1000, -200, -128, -1, 0, 1, 127, 128, 129, 1801, 1 << 30, (1 << 30) + 1):
         assert B.mx4_padded(cols) == B.lib.mx4_padded(cols), cols
     assert B.mx4_padded(-200) == 0 and B.mx4_padded(129) == 256
+
+
+def test_one_row_in_a_buffer_of_any_width(B):
+    """One token's microscaled form in the front of a longer buffer: nothing lies behind its row, so the buffer's width is no leading
+    dimension that the library could refuse (no multiple of 16 or 4 bytes, longer than 2^22)."""
+    import torch
+    u8 = torch.uint8
+    for per_q, per_s, cols in ((71, 5, 100), (64, 4, 128), (200, 7, 129), ((1 << 22) + 16, (1 << 22) + 4, 300)):
+        q, lds = B.Mx4(torch.zeros((1, per_q), dtype=u8), torch.zeros((1, per_s), dtype=u8), cols)._args()[1::2]
+        assert (q, lds) == (B.mx4_padded(cols) // 2, B.mx4_padded(cols) // 32)
+        # the checks let it pass: the call ends at the next one, the missing result
+        assert B.lib.mx4_dequantize(FAKE, q, FAKE, lds, 1, cols, B.DLA_F32, None, cols, None) == -8
