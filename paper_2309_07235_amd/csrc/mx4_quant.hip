@@ -80,10 +80,15 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t 
   typedef T run_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   __shared__ u32x4_t turned[128 * 4];
   __shared__ unsigned int scales[128];
-  // Workgroups go round the eight XCDs; where a row has 64 tiles, eight neighbours go to one, whose L2 then writes whole lines of q and s
-  // (8192 x 8192 bf16 45.5 us for 50.4, fp32 73 for 75; but 4096 x 4096 fp32, half as many tiles a row, 22.3 for 20.6).
+  // Workgroups go round the eight XCDs.  Two neighbours of a row of tiles share lines of q, two of a column lines of qt, and an L2 that
+  // has both writes them whole.  Where a row has a multiple of 64 tiles or up to two more or fewer, eight neighbours go to one XCD, and so does
+  // most often the tile below.  Time over that of the plain order, 4096 and 8192 rows: 62 to 66 tiles bf16 0.85 to 0.96, fp32 0.92 to 0.98, 127
+  // to 129 tiles 0.84 to 0.99 (1000 rows of 62 tiles 1.02 to 1.05, of 63 to 66 0.93 to 1.01).  Other numbers stay as they come: multiples of eight,
+  // whose columns are one XCD's already, 0.95 to 1.15 (the least of them 120 tiles of 8192 rows, 0.92), multiples of four 0.97 to 1.14; odd ones
+  // from 9 to 47 gain up to 0.88 in one type and size and nothing in the next.
   const unsigned int part = blockIdx.x / 64u * 64u, in = blockIdx.x % 64u;
-  const unsigned int id = tiles_c >= 64 && part + 64u <= gridDim.x ? part + in % 8u * 8u + in / 8u : blockIdx.x;
+  const bool near = tiles_c >= 62 && (tiles_c + 2) % 64 <= 4;
+  const unsigned int id = near && part + 64u <= gridDim.x ? part + in % 8u * 8u + in / 8u : blockIdx.x;
   const int64_t r0 = (int64_t)(id / (unsigned int)tiles_c) * 128, c0 = (int64_t)(id % (unsigned int)tiles_c) * 128;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4;
   const int64_t row = r0 + wave * 32 + group * 8, col = c0 + (lane & 15) * 8;

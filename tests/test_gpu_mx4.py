@@ -741,3 +741,17 @@ def test_apply_rows_at_every_alignment(B, dtype, op):
             announce(f"mx4_apply alignment {dtype} op {op} first {first} ldx {ldx}")
             B.mx4_apply(op, xd, w, y)
             assert np.array_equal(f64(y), want), (first, ldx)
+
+
+def test_quantize_widths_about_64_tiles(B):
+    """Rows of 61 to 67 and of 126 to 131 tiles: the numbers about a multiple of 64 at which the order of the tiles changes."""
+    rng = np.random.default_rng(25)
+    for tiles in (61, 62, 63, 64, 65, 66, 67, 126, 128, 130, 131):
+        rows, cols = (150, tiles * 128 - 5) if tiles < 100 else (129, tiles * 128)
+        announce(f"quantize {rows} x {cols}, {tiles} tiles a row")
+        x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-6, 7, (rows, cols)))
+        _, xd = put(x, "float32")
+        q, qt = room(B, rows, cols, 1), room(B, cols, rows, 1)
+        B.mx4_quantize(xd, q, qt)
+        check_form(q, f64(xd), 1)
+        check_form(qt, f64(xd).T, 1)
