@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(WV * 64) mx4_apply_direct_kernel(MxApplyArgs g
   const unsigned int at_w = lds_offset(ring), at_x = at_w + W_RING * 16, at_s = at_x + DX * X_STAGE * 16;
 
   // W: a load fills 16 rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4; X: 4 rows of 256 bytes, chunk c of row r at c ^ r % 16
+  // (a wave's read of 1 KB of either takes LDS 8 clocks; from neighbouring places 4)
   const uint8_t* const wq = g.w.q + (int64_t)n0 * g.w.ldq;
   const uint8_t* const ws = g.w.s + (int64_t)n0 * g.w.lds;
   const T* const x = static_cast<const T*>(g.x) + (int64_t)m0 * g.ldx;
@@ -423,7 +424,8 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_tile_kernel(MxApplyTile
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l31 = lane & 31, l5 = lane >> 5;
   const int wm0 = wave / WN * (TM / WM), wn0 = wave % WN * (TN / WN);
 
-  // X: a load fills eight rows, chunk c of row r at c ^ r / 2 % 8 (the 16 rows that are read at one chunk take all banks).  W: 32 rows.
+  // X: a load fills eight rows, chunk c of row r at c ^ r / 2 % 8 (a wave's read of 1 KB then takes LDS 4 clocks, as from neighbouring places).
+  // W: 32 rows of two chunks (8 clocks a read, and 8 for the scales, bytes 16 apart; of each there is one for four of X's or more).
   const __bf16* const xb = g.x + (int64_t)m0 * g.ldx + (int64_t)first * 64;
   const uint8_t* const wb = g.w.q + (int64_t)n0 * g.w.ldq + (int64_t)first * 32;
   unsigned int xoff[LX], woff[LW];
@@ -585,8 +587,9 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_apply_grad_kernel(MxApplyTile
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l31 = lane & 31, l5 = lane >> 5;
   const int wm0 = wave / WN * (TM / WM), wn0 = wave % WN * (TN / WN);
 
-  // Chunk c of 16 bytes of row r lies at c ^ turn(r): 16 rows that are read at the same chunk take all banks, and so do the
-  // columns 8 l + i that the lanes write.
+  // Chunk c of 16 bytes of row r lies at c ^ turn(r), so that neither rows that are read at the same chunk nor the columns 8 l + i that
+  // the lanes write lie in the same banks throughout.  It halves what LDS can do: a wave's read of 16 bytes a lane takes 8 clocks and its write
+  // of 8 bytes too, from neighbouring places 4 each (what is taken at a time is not 16 neighbouring lanes).
   auto turn = [](int r) { return ((r >> 1) ^ (r >> 3)) & 7; };
 
   // X: a load fills eight rows

@@ -35,7 +35,8 @@ __global__ void __launch_bounds__(WV * 64) mx4_gemm_direct_kernel(MxGemmArgs g) 
   u32x4_t* const ring = lds + wave * RING;
   const unsigned int at_q = lds_offset(ring), at_s = at_q + D * F * 1024;
 
-  // A's blocks of 16 rows, then B's.  A load fills one block's rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4.
+  // A's blocks of 16 rows, then B's.  A load fills one block's rows of 64 bytes, chunk c of row r at c ^ (r / 4) % 4 (a wave's read of them
+  // takes LDS 8 clocks; from neighbouring places 4).
   const uint8_t* const aq = g.a.q + (int64_t)m0 * g.a.ldq;
   const uint8_t* const bq = g.b.q + (int64_t)n0 * g.b.ldq;
   const uint8_t* const as = g.a.s + (int64_t)m0 * g.a.lds;
@@ -153,8 +154,9 @@ __global__ void __launch_bounds__(WM* WN * 64) mx4_gemm_tile_kernel(MxGemmArgs g
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l31 = lane & 31, l5 = lane >> 5;
   const int wm0 = wave / WN * (TM / WM), wn0 = wave % WN * (TN / WN);
 
-  // A load instruction fills 16 rows of 64 bytes; chunk c of row r lies at c ^ (r / 4) % 4, so that the 16 rows which a read of 16
-  // lanes takes lie in all banks.  Rows past the last repeat it.
+  // A load instruction fills 16 rows of 64 bytes; chunk c of row r lies at c ^ (r / 4) % 4, so that a wave's read of 32 rows takes LDS 4
+  // clocks, as from neighbouring places.  (The scales' reads, 4 bytes 16 apart, take 8, and 2 from neighbouring places: in a tile of 256 x 256
+  // six of them a step, which is as long as its twelve reads of operands.)  Rows past the last repeat it.
   const uint8_t* const aq = g.a.q + (int64_t)m0 * g.a.ldq + (int64_t)first * 64;
   const uint8_t* const bq = g.b.q + (int64_t)n0 * g.b.ldq + (int64_t)first * 64;
   unsigned int off[LA + LB];

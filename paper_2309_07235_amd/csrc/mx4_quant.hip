@@ -156,8 +156,8 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t 
     sc[4 * h + 3] = c3l;
     reinterpret_cast<uint8_t*>(scales)[((lane & 15) * 8 + 4 * h + (group >> 1) * 2 + (group & 1)) * 4 + wave] = (uint8_t)own;
   }
-  // A column's 64 bytes are put together in LDS: column 8 l + j at slot 16 j + l, wave w's 16 bytes of it at chunk w ^ l / 4, so that what
-  // a wave writes and reads at a time lies in all banks.
+  // A column's 64 bytes are put together in LDS: column 8 l + j at slot 16 j + l, wave w's 16 bytes of it at chunk w ^ l / 4.  A wave's read
+  // takes LDS 4 clocks, as from neighbouring places, its write of a dword 4 where it is 2 there.
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float c[8];

@@ -4,7 +4,8 @@
 
 namespace dla {
 
-// A tile and what a launch of it costs, in us: start + max(first + step * steps, each * (more + unit * steps)) for workgroups of `steps` times 128
+// A tile and what a launch of it costs, in us (at the clocks of short calls: a product of many tiles, for which the power that they draw brings
+// the clocks down, takes longer, 4096 x 8192 x 8192 of mx4_apply in bf16 414 to 430 us for 311 here; only the order of tiles counts): start + max(first + step * steps, each * (more + unit * steps)) for workgroups of `steps` times 128
 // terms, `each` of them to a compute unit (their number over 256, rounded up): the chain of one workgroup's steps, or the units' work.
 struct MxTileCost {
   int m, n;
