@@ -148,7 +148,7 @@ __device__ __forceinline__ float mx_again_down(const __bf16* x, int64_t plane, c
 // Few rows of X: what bounds the call is reading W once.  The WV waves of a workgroup share the sum over k, each with a run of
 // steps of 128 terms and LDS of its own, to which W is loaded DW steps ahead and X DX.  Through LDS, because the matrix instructions
 // want neighbouring lanes in different rows, and such a load takes 64 cycles where one of whole rows takes 16 (16384 x 4096 weights,
-// one row, bf16: 9.2 us, 3.9 TB/s; 16 us with loads to registers).  With 48 rows of fp16 by 8192 x 8192, 17.5 us, it is X too, which each of
+// one row, bf16: 9.2 us, 3.9 TB/s; 16 us with loads to registers).  With 48 rows of fp16 by 8192 x 8192, 16 to 18 us, it is X too, which each of
 // 256 workgroups reads, and the scaling of the products' sums.
 //   bf16, fp32   a lane's block of W is made bf16 with its scale; X is one plane of bf16 or, for fp32, three that add up to it (made by a
 //                launch in front: made here, by every workgroup, they cost more than the rest of the call); instruction b takes
@@ -403,7 +403,7 @@ constexpr int apply_depth(int tm, int tn, int terms) {
   return shared >= 3 ? (shared > 6 ? 6 : shared) : (alone > 4 ? 4 : alone);
 }
 
-// A tile of Y = X*W^T, bound by the bf16 matrix pipes and the power they draw: 4096 rows of bf16 by 8192 x 8192 in 418 us, 1310 TFLOP/s (a
+// A tile of Y = X*W^T, bound by the bf16 matrix pipes and the power they draw: 4096 rows of bf16 by 8192 x 8192 in 401 to 430 us by the clocks, 1320 TFLOP/s (a
 // library product of bf16 operands of 8192 x 8192 reaches 1410).  X's rows and W's go to LDS as they are, a ring of D steps of 64 terms; a wave makes its part of W bf16 as it
 // takes it to its registers (every element in WM waves).  A lane holds one block of a row of W, instruction j takes its elements
 // 8 j .. 8 j + 7, and X's likewise.
@@ -566,7 +566,7 @@ constexpr int grad_depth(int tm, int tn, int terms) {
   return shared >= 2 ? (shared > 4 ? 4 : shared) : (alone > 3 ? 3 : alone);
 }
 
-// A tile of Y = X*W: 2048 rows of bf16 by 8192 x 8192 in 236 us, 1170 TFLOP/s; what a thread does to turn W over takes issue slots from the
+// A tile of Y = X*W: 2048 rows of bf16 by 8192 x 8192 in 225 to 240 us by the clocks, 1180 TFLOP/s; what a thread does to turn W over takes issue slots from the
 // products.  X's rows and W's go to LDS as they are, a ring of D steps of 64 terms (rows of W).  The terms of the sum are the rows of W,
 // so what a lane needs of it is a column: a step ahead, threads turn blocks of 4 rows by 8 columns over in registers, make them bf16
 // and leave them in LDS with the terms as neighbours, once per workgroup.

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(WV * 64) mx4_gemm_direct_kernel(MxGemmArgs g) 
 // A tile.  An operation costs a quarter of bf16's here, an operand byte as much as ever: a tile of 256 x 256 takes 128 terms, 32 KB of
 // operands, in 1024 clocks of the matrix pipes, which is 32 bytes a clock into LDS and 96 out of it for eight waves of 128 x 64.  Hence
 // the largest tile the registers hold, operands that go to LDS without a register in between, four steps ahead, and LDS reads one half
-// step ahead, each between two products.  8192 x 8192, k = 8192: 288 us, 3.8 PFLOP/s (operands of zeros, for which the clocks stay up, 245 us).
+// step ahead, each between two products.  8192 x 8192, k = 8192: 276 to 290 us by the clocks, 3.8 PFLOP/s (operands of zeros, for which the clocks stay up, 245 us).
 // Tried and no better: more steps ahead, padded rows, loads to LDS between the products, four waves of 128 x 128, which read a third less
 // from LDS (313 us).  The tile of 128 x 128 is for results of few tiles: 1600 x 1800, k = 2000, fp32, in 10.4 us, operands in the caches.
 template <int TM, int TN, int WM, int WN, typename T>

@@ -72,8 +72,9 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* x, int64_t 
 // Across the rows, and along them too where q is given, a tile of 128 x 128 a workgroup.  A wave takes 32 rows, which are one block of every column,
 // a lane 8 x 8 of them: everything that belongs to one block is in 4 lanes, neighbours for a row's block, 16 apart for a
 // column's.  What a lane has for a column is eight rows' elements, a dword; they and the scales of the four waves meet in LDS.
-// Both forms of 8192 x 8192: fp32 73 us (4.7 TB/s), bf16 45.5 us (4.5 TB/s), X read once for the two; the tile itself through LDS, a
-// column's 32 rows then read by one lane, took 81 and 79.
+// Both forms of 8192 x 8192, X read once for the two and in no cache: fp32 67 us (5.1 TB/s), bf16 40 us (5.1 TB/s), call after call; 96 us (fp32) where
+// 500 MB that other kernels have just written are on their way to memory.  The tile itself through LDS, a column's 32 rows then read by one lane,
+// took 81 and 79 us where this took 73 and 46.
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* x, int64_t ldx, int64_t rows, int64_t cols, int tiles_c, uint8_t* q, int64_t ldq,
                                                             uint8_t* s, int64_t lds, uint8_t* qt, int64_t ldqt, uint8_t* st, int64_t ldst) {
